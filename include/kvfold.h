@@ -333,6 +333,63 @@ int kvfold_cache_profile_end(kvfold_cache_t* cache, int32_t* n_steps /* host */,
  */
 int kvfold_measure_peaks(int32_t device, double* mfma_bf16_tflops, double* hbm_read_gbps);
 
+/*
+ * ---- A cache held in 8 bits ------------------------------------------------------------------------------------------
+ * The same fold on a cache of about half the bytes of the bf16 one (the paper's Discussion, Sec. 8, asks what the carried cache
+ * survives; kvfold_cache_set_storage_roundtrip perturbs it, this one is stored so).  Rows [64 b, 64 b + 64) of a KV head are a block, which
+ * is held, once all of its rows are there, as whole numbers from -127 to 127 with one scale for K and one for V:
+ *        scale = max(max |x| / 127, 2^-100),  code = round-half-even(x / scale),
+ * quotients in fp32; the row that it stands for is code * scale.  Rows of the last, incomplete block are held as they came, in bf16, so that
+ * what the cache holds does not depend on the chunks that it was folded in.  Infinities are taken for the largest finite bf16 number of
+ * their sign, NaN for 0.  Keys are held rotated, as everywhere.
+ *
+ * The configuration is that of a cache, dtype KVFOLD_BF16 (else KVFOLD_ERR_UNSUPPORTED): q, k_new, v_new and out are bf16.  kv_buffer, if given,
+ * has kvfold_qcache_bytes_required() bytes.  Errors, streams and threads as for kvfold_cache_t: every error but KVFOLD_ERR_HIP is found before
+ * anything is enqueued, calls on one cache are issued from one thread at a time and stream-ordered, and nothing allocates or synchronises
+ * but create and destroy.
+ */
+typedef struct kvfold_qcache kvfold_qcache_t;
+
+/* Bytes of storage: codes, scales, and the bf16 rows of two blocks per layer and KV head.  Host-only; 0 for an invalid configuration. */
+size_t kvfold_qcache_bytes_required(const kvfold_config_t* cfg /* host */);
+int kvfold_qcache_create(const kvfold_config_t* cfg, kvfold_qcache_t** out_cache);
+int kvfold_qcache_destroy(kvfold_qcache_t* cache);
+
+/*
+ * One fold step on one layer, n_tokens in [1, cfg.chunk_tokens]: append the chunk's rows, then let query row i attend to the rows
+ * j <= pos_offset + i as the cache holds them after the append.  q, k_new, v_new, out, lse as for kvfold_step_ex; rope_cos and rope_sin as for
+ * kvfold_step_rope, or both NULL: q and k_new are used as given.  out may lie on q, k_new or v_new (in q's very place); any other
+ * overlap of out or lse with q, the angles, the cache's storage or one another is KVFOLD_ERR_INVALID_ARG.
+ */
+int kvfold_qcache_step(kvfold_qcache_t* cache, int layer, const void* q, const void* k_new, const void* v_new, int32_t n_tokens,
+                       int64_t pos_offset, const float* rope_cos, const float* rope_sin, void* out, float* lse, void* stream);
+
+/*
+ * Append without attention, any number of tokens that fits: to carry on in 8 bits what another cache holds, or to restore a fold.
+ *   k, v  device, bf16, 16-byte aligned: row t of KV head g begins token_stride * t + head_stride * g elements behind the pointer, both
+ *         multiples of 8 (kvfold_cache_view's row and head strides, say, or Hkv * d and d for [n][Hkv][d])
+ *   rope_cos, rope_sin  NULL, or the angles by which the K rows are rotated on their way, as for kvfold_step_rope
+ */
+int kvfold_qcache_append(kvfold_qcache_t* cache, int layer, const void* k, const void* v, int64_t token_stride, int64_t head_stride,
+                         int64_t n_tokens, int64_t pos_offset, const float* rope_cos, const float* rope_sin, void* stream);
+
+/*
+ * Rows [first, first + n_tokens) of `layer` as the numbers they stand for, code * scale (or the bf16 row) in fp32.
+ *   k_out, v_out  device, 16-byte aligned, [n_tokens][Hkv][d]; either may be NULL
+ * KVFOLD_ERR_POSITION for rows that the layer does not have.
+ */
+int kvfold_qcache_read(kvfold_qcache_t* cache, int layer, int64_t first, int64_t n_tokens, float* k_out, float* v_out, void* stream);
+
+/* Current number of rows held for `layer`; negative status on error.  Host-only. */
+int64_t kvfold_qcache_length(const kvfold_qcache_t* cache, int layer);
+
+/*
+ * Rewind `layer` (-1 = every layer) to `new_len` rows.  An incomplete block's rows have to be there in bf16: those of the last two blocks that
+ * rows were appended to are, so that at least the last 64 rows can be taken back to any place (and again, to where these two blocks begin);
+ * further back new_len must be a multiple of 64.  Else, or beyond the current length, KVFOLD_ERR_POSITION and nothing changes.  Host-only.
+ */
+int kvfold_qcache_truncate(kvfold_qcache_t* cache, int layer, int64_t new_len);
+
 /* Static, human-readable name of a status code. */
 const char* kvfold_status_string(int status);
 

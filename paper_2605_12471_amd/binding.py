@@ -109,6 +109,22 @@ def load_library() -> ctypes.CDLL:
     lib.kvfold_status_string.restype = ctypes.c_char_p
     lib.kvfold_measure_peaks.argtypes = [i32, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double)]
     lib.kvfold_measure_peaks.restype = ctypes.c_int
+    lib.kvfold_qcache_bytes_required.argtypes = [cfgp]
+    lib.kvfold_qcache_bytes_required.restype = ctypes.c_size_t
+    lib.kvfold_qcache_create.argtypes = [cfgp, ctypes.POINTER(vp)]
+    lib.kvfold_qcache_create.restype = ctypes.c_int
+    lib.kvfold_qcache_destroy.argtypes = [vp]
+    lib.kvfold_qcache_destroy.restype = ctypes.c_int
+    lib.kvfold_qcache_step.argtypes = [vp, ctypes.c_int, vp, vp, vp, i32, i64, vp, vp, vp, vp, vp]
+    lib.kvfold_qcache_step.restype = ctypes.c_int
+    lib.kvfold_qcache_append.argtypes = [vp, ctypes.c_int, vp, vp, i64, i64, i64, i64, vp, vp, vp]
+    lib.kvfold_qcache_append.restype = ctypes.c_int
+    lib.kvfold_qcache_read.argtypes = [vp, ctypes.c_int, i64, i64, vp, vp, vp]
+    lib.kvfold_qcache_read.restype = ctypes.c_int
+    lib.kvfold_qcache_length.argtypes = [vp, ctypes.c_int]
+    lib.kvfold_qcache_length.restype = i64
+    lib.kvfold_qcache_truncate.argtypes = [vp, ctypes.c_int, i64]
+    lib.kvfold_qcache_truncate.restype = ctypes.c_int
     lib.kvfold_last_hip_error.argtypes = []
     lib.kvfold_last_hip_error.restype = ctypes.c_int
     _lib = lib
@@ -218,6 +234,41 @@ def kvfold_cache_profile_end(cache):
     rc = load_library().kvfold_cache_profile_end(cache, ctypes.byref(n), ctypes.byref(a), ctypes.byref(t),
                                                  ctypes.byref(m))
     return rc, n.value, a.value, t.value, m.value
+
+
+def kvfold_qcache_bytes_required(cfg: kvfold_config_t) -> int:
+    return int(load_library().kvfold_qcache_bytes_required(ctypes.byref(cfg)))
+
+
+def kvfold_qcache_create(cfg: Optional[kvfold_config_t]):
+    """Returns (status, handle); handle is None on error."""
+    h = ctypes.c_void_p()
+    rc = load_library().kvfold_qcache_create(ctypes.byref(cfg) if cfg is not None else None, ctypes.byref(h))
+    return rc, (h if rc == 0 else None)
+
+
+def kvfold_qcache_destroy(cache) -> int:
+    return load_library().kvfold_qcache_destroy(cache)
+
+
+def kvfold_qcache_step(cache, layer, q, k_new, v_new, n_tokens, pos_offset, rope_cos, rope_sin, out, lse=None, stream=0) -> int:
+    return load_library().kvfold_qcache_step(cache, layer, q, k_new, v_new, n_tokens, pos_offset, rope_cos, rope_sin, out, lse, stream)
+
+
+def kvfold_qcache_append(cache, layer, k, v, token_stride, head_stride, n_tokens, pos_offset, rope_cos=None, rope_sin=None, stream=0) -> int:
+    return load_library().kvfold_qcache_append(cache, layer, k, v, token_stride, head_stride, n_tokens, pos_offset, rope_cos, rope_sin, stream)
+
+
+def kvfold_qcache_read(cache, layer, first, n_tokens, k_out, v_out, stream=0) -> int:
+    return load_library().kvfold_qcache_read(cache, layer, first, n_tokens, k_out, v_out, stream)
+
+
+def kvfold_qcache_length(cache, layer) -> int:
+    return int(load_library().kvfold_qcache_length(cache, layer))
+
+
+def kvfold_qcache_truncate(cache, layer, new_len) -> int:
+    return load_library().kvfold_qcache_truncate(cache, layer, new_len)
 
 
 def kvfold_status_string(status: int) -> str:
@@ -459,3 +510,115 @@ class KvFoldCache:
             return t if es == 4 else t.view(torch.bfloat16)
 
         return wrap(k), wrap(v)
+
+
+def _expect(name, t, dtype, device, shape=None, contiguous=True):
+    if not (t.is_cuda and t.get_device() == device):
+        raise ValueError(f"{name}: expected a tensor on cuda:{device}, got {t.device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: expected dtype {dtype}, got {t.dtype}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor")
+    return t.data_ptr()
+
+
+class KvFoldQuantCache:
+    """Owns one cache held in 8 bits (``kvfold_qcache_*``); bf16 torch tensors on the cache's device."""
+
+    def __init__(self, n_layers, n_q_heads, n_kv_heads, head_dim, chunk_tokens, capacity_tokens, softmax_scale=0.0, device=0):
+        import torch
+        self._bf16, self._f32 = torch.bfloat16, torch.float32
+        self.cfg = make_config(n_layers, n_q_heads, n_kv_heads, head_dim, chunk_tokens, capacity_tokens, KVFOLD_BF16, softmax_scale, device)
+        self.handle = None
+        rc, self.handle = kvfold_qcache_create(self.cfg)
+        if rc:
+            raise KvFoldError(rc, "kvfold_qcache_create")
+        self._device, self._hq, self._hkv, self._d = device, n_q_heads, n_kv_heads, head_dim
+        self._lib = load_library()
+
+    def close(self):
+        if getattr(self, "handle", None) is not None:
+            rc = kvfold_qcache_destroy(self.handle)
+            self.handle = None
+            if rc:
+                raise KvFoldError(rc, "kvfold_qcache_destroy")
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def _stream(self, stream):
+        if stream is not None:
+            return stream
+        import torch
+        return torch.cuda.current_stream(self._device).cuda_stream
+
+    def _angles(self, rope, n):
+        if rope is None:
+            return None, None
+        cos, sin = rope
+        return (_expect("rope cos", cos, self._f32, self._device, (n, self._d // 2)), _expect("rope sin", sin, self._f32, self._device, (n, self._d // 2)))
+
+    def step(self, layer, q, k_new, v_new, out, pos_offset=None, lse=None, stream=None, rope=None):
+        """Enqueue one fold step: q, out [n][Hq][d], k_new, v_new [n][Hkv][d], lse fp32 [Hq][n], all contiguous.  rope = (cos, sin), fp32
+        [n][d/2]: q and k_new are unrotated and the step rotates them."""
+        n = q.shape[0] if q.dim() == 3 else -1
+        wide, narrow = (n, self._hq, self._d), (n, self._hkv, self._d)
+        args = [_expect("q", q, self._bf16, self._device, wide), _expect("k_new", k_new, self._bf16, self._device, narrow),
+                _expect("v_new", v_new, self._bf16, self._device, narrow)]
+        cos, sin = self._angles(rope, n)
+        rc = self._lib.kvfold_qcache_step(self.handle, layer, *args, n, self.length(layer) if pos_offset is None else pos_offset, cos, sin,
+                                          _expect("out", out, self._bf16, self._device, wide),
+                                          None if lse is None else _expect("lse", lse, self._f32, self._device, (self._hq, n)), self._stream(stream))
+        if rc:
+            raise KvFoldError(rc, "kvfold_qcache_step")
+        return out
+
+    def append(self, layer, k, v, pos_offset=None, stream=None, rope=None):
+        """Append rows without attention: k, v [n][Hkv][d], any strides alike of both that are multiples of 8 elements, rows themselves
+        contiguous (``KvFoldCache.view(...)[:, :n].transpose(0, 1)``, say)."""
+        n = k.shape[0] if k.dim() == 3 else -1
+        for name, t in (("k", k), ("v", v)):
+            _expect(name, t, self._bf16, self._device, (n, self._hkv, self._d), contiguous=False)
+            if t.stride() != k.stride() or (n and t.stride(2) != 1):
+                raise ValueError(f"{name}: expected rows of stride 1 and the same strides for k and v, got {t.stride()}")
+        cos, sin = self._angles(rope, n)
+        rc = self._lib.kvfold_qcache_append(self.handle, layer, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), n,
+                                            self.length(layer) if pos_offset is None else pos_offset, cos, sin, self._stream(stream))
+        if rc:
+            raise KvFoldError(rc, "kvfold_qcache_append")
+
+    def read(self, layer, first, k_out, v_out, stream=None):
+        """Rows [first, first + n) as the fp32 numbers they stand for: k_out, v_out [n][Hkv][d] (either may be None)."""
+        given = [t for t in (k_out, v_out) if t is not None]
+        if not given:
+            return
+        n = given[0].shape[0] if given[0].dim() == 3 else -1
+        ptr = [None if t is None else _expect(name, t, self._f32, self._device, (n, self._hkv, self._d)) for name, t in (("k_out", k_out), ("v_out", v_out))]
+        rc = self._lib.kvfold_qcache_read(self.handle, layer, first, n, *ptr, self._stream(stream))
+        if rc:
+            raise KvFoldError(rc, "kvfold_qcache_read")
+
+    def bytes_required(self) -> int:
+        return kvfold_qcache_bytes_required(self.cfg)
+
+    def length(self, layer=0) -> int:
+        n = self._lib.kvfold_qcache_length(self.handle, layer)
+        if n < 0:
+            raise KvFoldError(n, "kvfold_qcache_length")
+        return n
+
+    def truncate(self, layer, new_len):
+        rc = self._lib.kvfold_qcache_truncate(self.handle, layer, new_len)
+        if rc:
+            raise KvFoldError(rc, "kvfold_qcache_truncate")

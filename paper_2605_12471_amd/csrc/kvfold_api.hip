@@ -22,18 +22,6 @@ using namespace kvfold;
 
 constexpr size_t kCounterBytes = (kMergeCounters + (size_t)kMeetUnits * kMeetStride) * sizeof(uint32_t);
 
-// Clears device memory and waits for it, on a stream that waits for no other and that none waits for: a cache may be created beside other streams'
-// work, or while one of them is being captured.  (46 us, and 350 in a process that has no other stream yet.)
-static hipError_t clear(void* p, size_t bytes) {
-  hipStream_t s;
-  hipError_t e = hipStreamCreateWithFlags(&s, hipStreamNonBlocking);
-  if (e != hipSuccess) return e;
-  e = hipMemsetAsync(p, 0, bytes, s);
-  const hipError_t done = hipStreamSynchronize(s);
-  (void)hipStreamDestroy(s);
-  return e != hipSuccess ? e : done;
-}
-
 struct kvfold_cache {
   PlanCtx pc;  // configuration, workspace size, CU count, tuning knobs, storage round trip: what the planner reads
   int elem_bytes;
@@ -63,6 +51,17 @@ int hip_fail(hipError_t e) {
   (void)hipGetLastError();  // clear the sticky error
   return e == hipErrorOutOfMemory ? KVFOLD_ERR_OOM : KVFOLD_ERR_HIP;
 }
+
+// (46 us, and 350 in a process that has no other stream yet.)
+hipError_t clear_device(void* p, size_t bytes) {
+  hipStream_t s;
+  hipError_t e = hipStreamCreateWithFlags(&s, hipStreamNonBlocking);
+  if (e != hipSuccess) return e;
+  e = hipMemsetAsync(p, 0, bytes, s);
+  const hipError_t done = hipStreamSynchronize(s);
+  (void)hipStreamDestroy(s);
+  return e != hipSuccess ? e : done;
+}
 }  // namespace kvfold
 
 namespace {
@@ -74,7 +73,6 @@ namespace {
 // comes from hipGetSymbolAddress, once per device.
 constexpr size_t kStaticScratchBytes = (size_t)kStaticScratchRows * (128 + 2) * sizeof(float);  // 65 MiB
 static __device__ __align__(256) unsigned char scratch[kStaticScratchBytes];
-constexpr int kMaxDevices = 64;
 unsigned char* g_scratch_ptr[kMaxDevices] = {};
 
 // Device address of this device's copy of the scratch array (the device must be current).
@@ -105,28 +103,6 @@ int take_counters(int device, uint32_t** out) {
   if (slot >= 0) *out = static_cast<uint32_t*>(ptr) + (size_t)slot * (kCounterBytes / sizeof(uint32_t));
   return slot;
 }
-
-// Whether two ranges of memory have no byte in common.
-bool apart(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x + a_bytes <= y || y + b_bytes <= x;
-}
-
-struct DeviceGuard {
-  int prev = -1;
-  bool switched = false;
-  hipError_t err = hipSuccess;
-  explicit DeviceGuard(int dev) {
-    err = hipGetDevice(&prev);
-    if (err == hipSuccess && prev != dev) {
-      err = hipSetDevice(dev);
-      switched = (err == hipSuccess);
-    }
-  }
-  ~DeviceGuard() {
-    if (switched) (void)hipSetDevice(prev);
-  }
-};
 
 }  // namespace
 
@@ -198,7 +174,7 @@ int kvfold_cache_create(const kvfold_config_t* cfg, kvfold_cache_t** out_cache) 
       c->counter_slot = take_counters(cfg->device, &c->merge_count);
       if (c->counter_slot < 0) {
         e = hipMalloc(&pc, kCounterBytes);
-        if (e == hipSuccess) e = clear(pc, kCounterBytes);
+        if (e == hipSuccess) e = clear_device(pc, kCounterBytes);
         c->merge_count = static_cast<uint32_t*>(pc);
       }
     }
