@@ -390,6 +390,46 @@ int64_t kvfold_qcache_length(const kvfold_qcache_t* cache, int layer);
  */
 int kvfold_qcache_truncate(kvfold_qcache_t* cache, int layer, int64_t new_len);
 
+/*
+ * ---- What the keys are worth, and keeping the best ---------------------------------------------------------------------
+ * The paper's cache only grows (Sec. 3) and the streaming baseline drops all but sinks and a window (Sec. 6); between the two a cache is cut down to the
+ * keys that attention has used.
+ *
+ * The softmax weight that the queries of the last n_tokens rows of `layer` gave to each of its keys, summed over rows and over the query heads
+ * of the KV head's group:
+ *        w[g][j] = sum over i, h of exp(scale * q[i][h] . K[g][j] - lse[h][i]),   j <= length - n_tokens + i.
+ * Called behind a step, with its q and the log-sum-exps that it left (kvfold_step_ex, _rope or _noalloc; those of kvfold_step_window are sums over
+ * fewer keys).  The weights of a KV head add up to n_tokens * Hq / Hkv.
+ *   q        device, [n_tokens][Hq][d], 1 <= n_tokens <= cfg.chunk_tokens
+ *   rope_cos, rope_sin  NULL, or the angles of the rows if q is unrotated, as for kvfold_step_rope
+ *   lse      device, [Hq][n_tokens]; a row whose lse is -inf counts for nothing
+ *   weights  device, [Hkv][capacity_tokens] float.  add = 0: entries [0, length) are set, add = 1: added to (which needs entries that begin
+ *            at zero); entries behind are left alone.  Apart from all inputs, else KVFOLD_ERR_INVALID_ARG.
+ * KVFOLD_ERR_POSITION if the layer has fewer than n_tokens rows.  The sums are fp32; the same call gives the same bits.
+ */
+int kvfold_cache_weigh(kvfold_cache_t* cache, int layer, const void* q, int32_t n_tokens, const float* rope_cos, const float* rope_sin,
+                       const float* lse, float* weights, int32_t add, void* stream);
+
+/* Bytes of device memory that kvfold_cache_evict needs for n_keep rows.  Host-only; 0 for an invalid n_keep. */
+size_t kvfold_evict_workspace_bytes(const kvfold_cache_t* cache, int64_t n_keep);
+
+/*
+ * Keep n_keep rows of `layer` per KV head: the first n_sink, the last n_recent and, of those between, the ones with the largest weights (NaN counts
+ * as the largest, equal weights by the lowest index).  They keep their order and become rows [0, n_keep) of layer `to_layer` of `to`, a
+ * cache of the same heads, type and device (else KVFOLD_ERR_UNSUPPORTED), or of the layer itself: to = NULL.  That layer's length becomes n_keep; another
+ * layer that rows are taken from stays as it is.  Keys stay rotated to the positions that they were appended at, and different heads keep
+ * different tokens; pos_offset of later steps counts rows, the angles of new tokens are the caller's as before.
+ *   weights     device, [Hkv][capacity of cache] float: kvfold_cache_weigh's, say
+ *   to_weights  device or NULL, [Hkv][capacity of to] float: receives the kept rows' weights and zero behind them; may be `weights`
+ *   kept        device or NULL, [Hkv][n_keep]: receives the kept rows' indices, ascending
+ *   workspace   device, 4-byte aligned, kvfold_evict_workspace_bytes() bytes (else KVFOLD_ERR_OOM), the call's own until the stream has passed it; needs no
+ *               initial contents
+ * 1 <= n_keep, n_sink + n_recent <= n_keep, else KVFOLD_ERR_INVALID_ARG; n_keep beyond the length KVFOLD_ERR_POSITION, beyond the target's
+ * capacity KVFOLD_ERR_CAPACITY.  Overlaps other than those named are KVFOLD_ERR_INVALID_ARG.
+ */
+int kvfold_cache_evict(kvfold_cache_t* cache, int layer, const float* weights, int64_t n_keep, int64_t n_sink, int64_t n_recent, kvfold_cache_t* to,
+                       int to_layer, float* to_weights, int32_t* kept, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Static, human-readable name of a status code. */
 const char* kvfold_status_string(int status);
 

@@ -125,6 +125,12 @@ def load_library() -> ctypes.CDLL:
     lib.kvfold_qcache_length.restype = i64
     lib.kvfold_qcache_truncate.argtypes = [vp, ctypes.c_int, i64]
     lib.kvfold_qcache_truncate.restype = ctypes.c_int
+    lib.kvfold_cache_weigh.argtypes = [vp, ctypes.c_int, vp, i32, vp, vp, vp, vp, i32, vp]
+    lib.kvfold_cache_weigh.restype = ctypes.c_int
+    lib.kvfold_evict_workspace_bytes.argtypes = [vp, i64]
+    lib.kvfold_evict_workspace_bytes.restype = ctypes.c_size_t
+    lib.kvfold_cache_evict.argtypes = [vp, ctypes.c_int, vp, i64, i64, i64, vp, ctypes.c_int, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.kvfold_cache_evict.restype = ctypes.c_int
     lib.kvfold_last_hip_error.argtypes = []
     lib.kvfold_last_hip_error.restype = ctypes.c_int
     _lib = lib
@@ -236,6 +242,18 @@ def kvfold_cache_profile_end(cache):
     return rc, n.value, a.value, t.value, m.value
 
 
+def kvfold_cache_weigh(cache, layer, q, n_tokens, rope_cos, rope_sin, lse, weights, add=0, stream=0) -> int:
+    return load_library().kvfold_cache_weigh(cache, layer, q, n_tokens, rope_cos, rope_sin, lse, weights, add, stream)
+
+
+def kvfold_evict_workspace_bytes(cache, n_keep) -> int:
+    return int(load_library().kvfold_evict_workspace_bytes(cache, n_keep))
+
+
+def kvfold_cache_evict(cache, layer, weights, n_keep, n_sink, n_recent, to, to_layer, to_weights, kept, workspace, workspace_bytes, stream=0) -> int:
+    return load_library().kvfold_cache_evict(cache, layer, weights, n_keep, n_sink, n_recent, to, to_layer, to_weights, kept, workspace, workspace_bytes, stream)
+
+
 def kvfold_qcache_bytes_required(cfg: kvfold_config_t) -> int:
     return int(load_library().kvfold_qcache_bytes_required(ctypes.byref(cfg)))
 
@@ -337,7 +355,7 @@ class KvFoldCache:
         if rc:
             raise KvFoldError(rc, "kvfold_cache_create")
         # what every step needs, as plain Python values: fields of a ctypes structure are slow to read
-        self._device, self._hq, self._hkv, self._d = device, n_q_heads, n_kv_heads, head_dim
+        self._device, self._hq, self._hkv, self._d, self._capacity = device, n_q_heads, n_kv_heads, head_dim, capacity_tokens
         self._lib = load_library()
         self._bound = False  # what the native step knows of this cache; None: there is none
 
@@ -444,6 +462,54 @@ class KvFoldCache:
         if rc:
             raise KvFoldError(rc, "kvfold_step_rope")
         return out
+
+    def weigh(self, layer, q, lse, weights, add=True, rope=None, stream=None):
+        """Enqueue kvfold_cache_weigh behind a step: its q [n][Hq][d] and the lse [Hq][n] that it left; weights fp32 [Hkv][capacity], added to or
+        (add=False) set.  rope = (cos, sin), fp32 [n][d/2]: q is unrotated.  Returns weights."""
+        import torch
+        f32, shape = torch.float32, q.shape
+        n = shape[0] if len(shape) == 3 else -1
+        self._check("q", q, (n, self._hq, self._d))
+        self._check("lse", lse, (self._hq, n), f32)
+        self._check("weights", weights, (self._hkv, self._capacity), f32)
+        cos = sin = None
+        if rope is not None:
+            cos, sin = rope
+            self._check("rope cos", cos, (n, self._d // 2), f32)
+            self._check("rope sin", sin, (n, self._d // 2), f32)
+            cos, sin = cos.data_ptr(), sin.data_ptr()
+        rc = self._lib.kvfold_cache_weigh(self.handle, layer, q.data_ptr(), n, cos, sin, lse.data_ptr(), weights.data_ptr(), 1 if add else 0, self._stream(stream))
+        if rc:
+            raise KvFoldError(rc, "kvfold_cache_weigh")
+        return weights
+
+    def evict(self, layer, weights, n_keep, n_sink=0, n_recent=0, to=None, to_layer=0, to_weights=None, kept=None, workspace=None, stream=None):
+        """Enqueue kvfold_cache_evict: per KV head the first n_sink rows, the last n_recent and the heaviest between them, n_keep in all, move
+        to the front of this layer or to layer to_layer of the cache `to`.  weights fp32 [Hkv][capacity]; to_weights fp32 [Hkv][capacity of the
+        target]; kept int32 [Hkv][n_keep], made here if not given, and returned.  workspace: a uint8 tensor of evict_workspace_bytes(n_keep), else one
+        is made, which takes the memory pool of torch's current stream: with `stream` given, hand in a workspace and kept of that stream."""
+        import torch
+        target = self if to is None else to
+        self._check("weights", weights, (self._hkv, self._capacity), torch.float32)
+        if to_weights is not None:
+            self._check("to_weights", to_weights, (self._hkv, target._capacity), torch.float32)
+        need = kvfold_evict_workspace_bytes(self.handle, n_keep)
+        if kept is None:
+            kept = torch.empty((self._hkv, max(n_keep, 0)), dtype=torch.int32, device=weights.device)
+        self._check("kept", kept, (self._hkv, n_keep), torch.int32)
+        if workspace is None:
+            workspace = torch.empty((max(need, 4),), dtype=torch.uint8, device=weights.device)
+        else:
+            self._check("workspace", workspace, (workspace.numel(),), torch.uint8)
+        rc = self._lib.kvfold_cache_evict(self.handle, layer, weights.data_ptr(), n_keep, n_sink, n_recent, None if to is None else to.handle, to_layer,
+                                          None if to_weights is None else to_weights.data_ptr(), kept.data_ptr(), workspace.data_ptr(),
+                                          workspace.numel(), self._stream(stream))
+        if rc:
+            raise KvFoldError(rc, "kvfold_cache_evict")
+        return kept
+
+    def evict_workspace_bytes(self, n_keep) -> int:
+        return kvfold_evict_workspace_bytes(self.handle, n_keep)
 
     def bytes_required(self) -> int:
         return kvfold_cache_bytes_required(self.cfg)

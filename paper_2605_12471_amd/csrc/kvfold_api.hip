@@ -17,6 +17,7 @@
 #include "../../include/kvfold.h"
 #include "kvfold_host.h"
 #include "kvfold_internal.h"
+#include "weigh.h"
 
 using namespace kvfold;
 
@@ -582,6 +583,124 @@ int kvfold_cache_profile_end(kvfold_cache_t* c, int32_t* n_steps, double* append
   c->prof_max_steps = 0;
   c->prof_steps = 0;
   return rc;
+}
+
+int kvfold_cache_weigh(kvfold_cache_t* c, int layer, const void* q, int32_t n_tokens, const float* rope_cos, const float* rope_sin, const float* lse,
+                       float* weights, int32_t add, void* stream) {
+  if (!c || !q || !lse || !weights || (rope_cos == nullptr) != (rope_sin == nullptr) || (add & ~1)) return KVFOLD_ERR_INVALID_ARG;
+  const kvfold_config_t& f = c->pc.cfg;
+  if (layer < 0 || layer >= f.n_layers) return KVFOLD_ERR_BAD_LAYER;
+  if (n_tokens < 1 || n_tokens > f.chunk_tokens) return KVFOLD_ERR_INVALID_ARG;
+  const int64_t len = c->len[(size_t)layer];
+  if (n_tokens > len) return KVFOLD_ERR_POSITION;
+  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(rope_cos) | reinterpret_cast<uintptr_t>(rope_sin)) & 15 ||
+      (reinterpret_cast<uintptr_t>(lse) | reinterpret_cast<uintptr_t>(weights)) & 3)
+    return KVFOLD_ERR_INVALID_ARG;
+  const size_t weight_bytes = (size_t)f.n_kv_heads * (size_t)f.capacity_tokens * sizeof(float), rows = (size_t)n_tokens * f.n_q_heads;
+  const size_t angles = (size_t)n_tokens * (f.head_dim / 2) * sizeof(float);
+  if (!apart(weights, weight_bytes, q, rows * f.head_dim * c->elem_bytes) || !apart(weights, weight_bytes, lse, rows * sizeof(float)) ||
+      !apart(weights, weight_bytes, c->kv, c->kv_bytes) || (rope_cos && (!apart(weights, weight_bytes, rope_cos, angles) || !apart(weights, weight_bytes, rope_sin, angles))))
+    return KVFOLD_ERR_INVALID_ARG;
+  DeviceGuard guard(f.device);
+  if (guard.err != hipSuccess) return hip_fail(guard.err);
+  const size_t layer_block = (size_t)f.n_kv_heads * (size_t)f.capacity_tokens * (size_t)f.head_dim * c->elem_bytes;
+  WeighParams p;
+  p.q = q;
+  p.k = c->kv + (size_t)layer * layer_block;
+  p.lse = lse;
+  p.weights = weights;
+  p.rope_cos = rope_cos;
+  p.rope_sin = rope_sin;
+  p.capacity = f.capacity_tokens;
+  p.n_tokens = n_tokens;
+  p.n_q_heads = f.n_q_heads;
+  p.n_kv_heads = f.n_kv_heads;
+  p.group = f.n_q_heads / f.n_kv_heads;
+  p.len = (int32_t)len;
+  p.add = add;
+  p.scale_log2e = std::max(c->scale * 1.4426950408889634f, 0x1p-126f);  // (above 0: it multiplies -inf where a key is not seen)
+  p.by_group = fast_div(p.group);
+  const hipError_t e = launch_weigh(p, f.head_dim, f.dtype == KVFOLD_BF16, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? KVFOLD_OK : hip_fail(e);
+}
+
+size_t kvfold_evict_workspace_bytes(const kvfold_cache_t* c, int64_t n_keep) {
+  if (!c || n_keep < 1 || n_keep > c->pc.cfg.capacity_tokens) return 0;
+  return evict_layout(c->pc.cfg.n_kv_heads, n_keep).words * sizeof(uint32_t);
+}
+
+int kvfold_cache_evict(kvfold_cache_t* c, int layer, const float* weights, int64_t n_keep, int64_t n_sink, int64_t n_recent, kvfold_cache_t* to,
+                       int to_layer, float* to_weights, int32_t* kept, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!c || !weights || !workspace || n_keep < 1 || n_sink < 0 || n_recent < 0 || n_sink > n_keep || n_recent > n_keep - n_sink) return KVFOLD_ERR_INVALID_ARG;
+  if (!to) {
+    to = c;
+    to_layer = layer;
+  }
+  const kvfold_config_t &f = c->pc.cfg, &t = to->pc.cfg;
+  if (layer < 0 || layer >= f.n_layers || to_layer < 0 || to_layer >= t.n_layers) return KVFOLD_ERR_BAD_LAYER;
+  const int64_t len = c->len[(size_t)layer];
+  if (n_keep > len) return KVFOLD_ERR_POSITION;
+  if (t.device != f.device || t.n_kv_heads != f.n_kv_heads || t.head_dim != f.head_dim || t.dtype != f.dtype) return KVFOLD_ERR_UNSUPPORTED;
+  if (n_keep > t.capacity_tokens) return KVFOLD_ERR_CAPACITY;
+  const bool in_place = to == c && to_layer == layer;
+  const EvictLayout ws = evict_layout(f.n_kv_heads, n_keep);
+  if (workspace_bytes < ws.words * sizeof(uint32_t)) return KVFOLD_ERR_OOM;
+  if ((reinterpret_cast<uintptr_t>(weights) | reinterpret_cast<uintptr_t>(to_weights) | reinterpret_cast<uintptr_t>(kept) | reinterpret_cast<uintptr_t>(workspace)) & 3)
+    return KVFOLD_ERR_INVALID_ARG;
+  const size_t row_bytes = (size_t)f.head_dim * c->elem_bytes;
+  const size_t from_block = (size_t)f.n_kv_heads * (size_t)f.capacity_tokens * row_bytes, to_block = (size_t)f.n_kv_heads * (size_t)t.capacity_tokens * row_bytes;
+  unsigned char *from_rows[2], *to_rows[2];
+  for (int v = 0; v < 2; ++v) {
+    from_rows[v] = c->kv + (v ? c->kv_bytes / 2 : 0) + (size_t)layer * from_block;
+    to_rows[v] = to->kv + (v ? to->kv_bytes / 2 : 0) + (size_t)to_layer * to_block;
+  }
+  // Everything that is written lies apart from all else, but for to_weights in the place of weights, which are read by the first kernel only.
+  struct Range {
+    const void* at;
+    size_t bytes;
+  };
+  const Range in[] = {{weights, (size_t)f.n_kv_heads * (size_t)f.capacity_tokens * sizeof(float)}, {from_rows[0], from_block}, {from_rows[1], from_block}};
+  const Range out[] = {{workspace, ws.words * sizeof(uint32_t)},
+                       {kept, kept ? (size_t)f.n_kv_heads * (size_t)n_keep * sizeof(int32_t) : 0},
+                       {to_weights, to_weights ? (size_t)f.n_kv_heads * (size_t)t.capacity_tokens * sizeof(float) : 0},
+                       {to_rows[0], to_block},
+                       {to_rows[1], to_block}};
+  bool ok = true;
+  for (int i = 0; i < 5; ++i) {
+    if (!out[i].bytes) continue;
+    for (int j = 0; j < 3; ++j) {
+      const bool own_rows = in_place && i >= 3 && j >= 1, own_weights = i == 2 && j == 0;
+      ok = ok && (own_rows || own_weights || apart(out[i].at, out[i].bytes, in[j].at, in[j].bytes));
+    }
+    for (int j = 0; j < i; ++j) ok = ok && (!out[j].bytes || apart(out[i].at, out[i].bytes, out[j].at, out[j].bytes));
+  }
+  if (!ok) return KVFOLD_ERR_INVALID_ARG;
+
+  DeviceGuard guard(f.device);
+  if (guard.err != hipSuccess) return hip_fail(guard.err);
+  EvictParams p;
+  p.weights = weights;
+  for (int v = 0; v < 2; ++v) {
+    p.from[v] = from_rows[v];
+    p.to[v] = to_rows[v];
+  }
+  p.to_weights = to_weights;
+  p.workspace = static_cast<uint32_t*>(workspace);
+  p.kept = kept ? kept : reinterpret_cast<int32_t*>(p.workspace + ws.kept);
+  p.ws = ws;
+  p.from_capacity = f.capacity_tokens;
+  p.to_capacity = t.capacity_tokens;
+  p.n_kv_heads = f.n_kv_heads;
+  p.row_bytes = (int32_t)row_bytes;
+  p.len = (int32_t)len;
+  p.n_sink = (int32_t)n_sink;
+  p.n_recent = (int32_t)n_recent;
+  p.n_keep = (int32_t)n_keep;
+  p.in_place = in_place;
+  const hipError_t e = launch_evict(p, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e);
+  to->len[(size_t)to_layer] = n_keep;
+  return KVFOLD_OK;
 }
 
 int kvfold_last_hip_error(void) { return g_last_hip_error; }

@@ -1,0 +1,65 @@
+// Attention weights by key, and the eviction of keys by them (kvfold_cache_weigh, kvfold_cache_evict).
+#pragma once
+#include <stddef.h>
+#include <stdint.h>
+
+namespace kvfold {
+
+constexpr int kEvictRows = 64;  // rows that a workgroup moves
+
+// The caller's workspace of an eviction, in words: kept rows' indices and weights [Hkv][n_keep], per chunk of kEvictRows rows the number of kept
+// rows in front of it [Hkv][chunks + 1] and whether its rows have been read [Hkv][chunks], the next chunk to move.
+struct EvictLayout {
+  int64_t chunks;
+  size_t kept, weights, before, read, next, words;
+};
+inline EvictLayout evict_layout(int64_t n_kv_heads, int64_t n_keep) {
+  EvictLayout l;
+  l.chunks = (n_keep + kEvictRows - 1) / kEvictRows;
+  const size_t rows = (size_t)(n_kv_heads * n_keep), chunks = (size_t)(n_kv_heads * l.chunks);
+  l.kept = 0;
+  l.weights = l.kept + rows;
+  l.before = l.weights + rows;
+  l.read = l.before + chunks + (size_t)n_kv_heads;
+  l.next = l.read + chunks;
+  l.words = l.next + 1;
+  return l;
+}
+
+}  // namespace kvfold
+
+#if defined(__HIP__)
+#include "kvfold_internal.h"
+
+namespace kvfold {
+
+struct WeighParams {
+  const void* q;       // [n][Hq][d]
+  const void* k;       // layer base, [Hkv][cap][d]
+  const float* lse;    // [Hq][n], natural logarithms
+  float* weights;      // [Hkv][cap]
+  const float *rope_cos, *rope_sin;  // of the queries, [n][d/2], or nullptr
+  int64_t capacity;
+  int32_t n_tokens, n_q_heads, n_kv_heads, group, len;  // len: rows of the layer, the chunk's n_tokens the last of them
+  int32_t add;
+  float scale_log2e;
+  FastDiv by_group;
+};
+hipError_t launch_weigh(const WeighParams& p, int head_dim, bool bf16, hipStream_t s);
+
+struct EvictParams {
+  const float* weights;     // [Hkv][from_capacity]
+  const unsigned char* from[2];  // K, V: layer base, [Hkv][from_capacity][row_bytes]
+  unsigned char* to[2];
+  float* to_weights;        // [Hkv][to_capacity] or nullptr
+  int32_t* kept;            // [Hkv][n_keep]
+  uint32_t* workspace;
+  EvictLayout ws;
+  int64_t from_capacity, to_capacity;
+  int32_t n_kv_heads, row_bytes, len, n_sink, n_recent, n_keep;
+  int32_t in_place;
+};
+hipError_t launch_evict(const EvictParams& p, hipStream_t s);
+
+}  // namespace kvfold
+#endif
