@@ -194,6 +194,8 @@ def prepare(case, seed):
         if own:
             to = KvFoldCache(1, hq, hkv, d, min(keep, 256), keep, case["dtype"])
             state["to"], state["to_rows"] = to, to.view(0)
+            for rows in state["to_rows"]:
+                rows.owner = to  # the view aliases the cache's memory: whoever holds the rows keeps the cache
         else:
             state["k_rows"], state["v_rows"] = (x[name].transpose(0, 1).contiguous() for name in ("k_prev", "v_prev"))
     del x["k_prev"], x["v_prev"]
