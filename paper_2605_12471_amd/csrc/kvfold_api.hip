@@ -626,7 +626,7 @@ int kvfold_cache_weigh(kvfold_cache_t* c, int layer, const void* q, int32_t n_to
 
 size_t kvfold_evict_workspace_bytes(const kvfold_cache_t* c, int64_t n_keep) {
   if (!c || n_keep < 1 || n_keep > c->pc.cfg.capacity_tokens) return 0;
-  return evict_layout(c->pc.cfg.n_kv_heads, n_keep).words * sizeof(uint32_t);
+  return evict_layout(c->pc.cfg.n_kv_heads, n_keep, c->pc.cfg.capacity_tokens).words * sizeof(uint32_t);
 }
 
 int kvfold_cache_evict(kvfold_cache_t* c, int layer, const float* weights, int64_t n_keep, int64_t n_sink, int64_t n_recent, kvfold_cache_t* to,
@@ -643,7 +643,7 @@ int kvfold_cache_evict(kvfold_cache_t* c, int layer, const float* weights, int64
   if (t.device != f.device || t.n_kv_heads != f.n_kv_heads || t.head_dim != f.head_dim || t.dtype != f.dtype) return KVFOLD_ERR_UNSUPPORTED;
   if (n_keep > t.capacity_tokens) return KVFOLD_ERR_CAPACITY;
   const bool in_place = to == c && to_layer == layer;
-  const EvictLayout ws = evict_layout(f.n_kv_heads, n_keep);
+  const EvictLayout ws = evict_layout(f.n_kv_heads, n_keep, f.capacity_tokens);
   if (workspace_bytes < ws.words * sizeof(uint32_t)) return KVFOLD_ERR_OOM;
   if ((reinterpret_cast<uintptr_t>(weights) | reinterpret_cast<uintptr_t>(to_weights) | reinterpret_cast<uintptr_t>(kept) | reinterpret_cast<uintptr_t>(workspace)) & 3)
     return KVFOLD_ERR_INVALID_ARG;

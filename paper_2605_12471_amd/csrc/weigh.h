@@ -5,24 +5,31 @@
 
 namespace kvfold {
 
-constexpr int kEvictRows = 64;  // rows that a workgroup moves
+constexpr int kEvictRows = 64;     // rows that a workgroup moves
+constexpr int kEvictPiece = 8192;  // rows that a workgroup looks through where a KV head has several
 
 // The caller's workspace of an eviction, in words: kept rows' indices and weights [Hkv][n_keep], per chunk of kEvictRows rows the number of kept
-// rows in front of it [Hkv][chunks + 1] and whether its rows have been read [Hkv][chunks], the next chunk to move.
+// rows in front of it [Hkv][chunks + 1] and whether its rows have been read [Hkv][chunks], the next chunk to move; for pieces of long
+// caches the counts of a digit's values [2][Hkv][pieces][256], the rows known to be kept [Hkv][pieces], and what is known of the smallest kept
+// weight [2][Hkv][2].
 struct EvictLayout {
-  int64_t chunks;
-  size_t kept, weights, before, read, next, words;
+  int64_t chunks, pieces;
+  size_t kept, weights, before, read, next, counts, more, state, words;
 };
-inline EvictLayout evict_layout(int64_t n_kv_heads, int64_t n_keep) {
+inline EvictLayout evict_layout(int64_t n_kv_heads, int64_t n_keep, int64_t capacity) {
   EvictLayout l;
   l.chunks = (n_keep + kEvictRows - 1) / kEvictRows;
+  l.pieces = (capacity + kEvictPiece - 1) / kEvictPiece;
   const size_t rows = (size_t)(n_kv_heads * n_keep), chunks = (size_t)(n_kv_heads * l.chunks);
   l.kept = 0;
   l.weights = l.kept + rows;
   l.before = l.weights + rows;
   l.read = l.before + chunks + (size_t)n_kv_heads;
   l.next = l.read + chunks;
-  l.words = l.next + 1;
+  l.counts = l.next + 1;
+  l.more = l.counts + 2 * 256 * (size_t)(n_kv_heads * l.pieces);
+  l.state = l.more + (size_t)(n_kv_heads * l.pieces);
+  l.words = l.state + 4 * (size_t)n_kv_heads;
   return l;
 }
 

@@ -20,11 +20,13 @@ using namespace kvfold;
 
 static void layout() {
   for (int64_t heads : {1, 3, 8})
-    for (int64_t keep : {1, 63, 64, 65, 1000}) {
-      const EvictLayout l = evict_layout(heads, keep);
+    for (int64_t keep : {1, 63, 64, 65, 1000, 20000}) {
+      const EvictLayout l = evict_layout(heads, keep, keep + 500);
       CHECK(l.chunks * kEvictRows >= keep && (l.chunks - 1) * kEvictRows < keep);
       CHECK(l.weights == l.kept + (size_t)(heads * keep) && l.before == l.weights + (size_t)(heads * keep));
-      CHECK(l.read == l.before + (size_t)(heads * (l.chunks + 1)) && l.next == l.read + (size_t)(heads * l.chunks) && l.words == l.next + 1);
+      CHECK(l.read == l.before + (size_t)(heads * (l.chunks + 1)) && l.next == l.read + (size_t)(heads * l.chunks) && l.counts == l.next + 1);
+      CHECK(l.pieces * kEvictPiece >= keep + 500 && l.more == l.counts + (size_t)(512 * heads * l.pieces) && l.state == l.more + (size_t)(heads * l.pieces));
+      CHECK(l.words == l.state + (size_t)(4 * heads));
     }
 }
 

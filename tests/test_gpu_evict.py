@@ -234,6 +234,14 @@ def test_a_long_cache(where, keep):
     run_evict(cache, k, v, some_weights(8, 40000, 1, "plain"), keep, 4, 256, keep + 100, where)
 
 
+@pytest.mark.parametrize("kind", ["plain", "ties", "equal", "odd"])
+@pytest.mark.parametrize("length,keep,sink,recent", [(4096, 4000, 0, 0), (4097, 1, 0, 0), (8192, 100, 4, 8), (8193, 8192, 0, 0), (8193, 70, 60, 10), (16384, 9000, 8200, 5),
+                                                     (20000, 16000, 0, 9000), (25000, 25000, 0, 0), (25000, 8300, 0, 8300), (33000, 12000, 1, 1)])
+def test_rows_looked_through_by_one_or_several(kind, length, keep, sink, recent):
+    cache, k, v = filled(2, 2, 64, length)
+    run_evict(cache, k, v, some_weights(2, length, length, kind), keep, sink, recent, keep, "here")
+
+
 @pytest.mark.parametrize("first", [True, False])
 def test_the_kept_rows_are_the_first_or_the_last(first):
     """Nothing moves, or everything does, as far as it can."""
