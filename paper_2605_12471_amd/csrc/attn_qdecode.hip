@@ -73,20 +73,26 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attn_qdecode_kernel(QAttnParam
   const int key_row = 32 * (c16 >> 3) + 4 * (c16 >> 2 & 1) + (c16 & 3), key_mine = 32 * (kg >> 1) + 4 * (kg & 1);
   const unsigned k_lane = (unsigned)q_k_piece(kg, key_row) * 16, v_lane = (unsigned)q_v_piece(D, kg, c16) * 16;
 
+  // Blocks come by buffer loads: a lane's place in a block is fixed, the block's is a scalar, and a block that does not exist (past the last) is asked for in
+  // an empty buffer, which costs no traffic, so that the loads in flight are the same on every path and the compiler can count them.
   struct Codes {
     quintx4 k[4][H], v[J];
     floatx2 scale;
   };
-  auto load = [&](Codes& x, int b) __attribute__((always_inline)) {
-    const unsigned char* kb = kcodes + (uint64_t)(unsigned)b * BLOCK;
-    const unsigned char* vb = vcodes + (uint64_t)(unsigned)b * BLOCK;
-    x.scale = *reinterpret_cast<const floatx2*>(scales + 2 * (unsigned)b);
+  const unsigned head_bytes = (unsigned)qp.c.blocks * (unsigned)BLOCK;  // (at most 2^31: half of what the rows may take in bf16)
+  auto load = [&](Codes& x, int b, bool there) __attribute__((always_inline)) {
+    const __amdgpu_buffer_rsrc_t kb = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(kcodes), 0, there ? head_bytes : 0u, kRawBuffer);
+    const __amdgpu_buffer_rsrc_t vb = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(vcodes), 0, there ? head_bytes : 0u, kRawBuffer);
+    const __amdgpu_buffer_rsrc_t sb = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(scales), 0, there ? (unsigned)qp.c.blocks * 8u : 0u, kRawBuffer);
+    const unsigned at = (unsigned)b * (unsigned)BLOCK;
+    x.scale = __builtin_bit_cast(floatx2, __builtin_amdgcn_raw_buffer_load_b64(sb, 0, (unsigned)b * 8u, 0));
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int h = 0; h < H; ++h) x.k[t][h] = *reinterpret_cast<const quintx4*>(kb + k_lane + (unsigned)(q_k_piece(4 * h, 8 * t) * 16));
+      for (int h = 0; h < H; ++h)
+        x.k[t][h] = __builtin_bit_cast(quintx4, __builtin_amdgcn_raw_buffer_load_b128(kb, k_lane + (unsigned)(q_k_piece(4 * h, 8 * t) * 16), at, 0));
 #pragma unroll
-    for (int j = 0; j < J; ++j) x.v[j] = *reinterpret_cast<const quintx4*>(vb + v_lane + (unsigned)(q_v_piece(D, 0, 16 * j) * 16));
+    for (int j = 0; j < J; ++j) x.v[j] = __builtin_bit_cast(quintx4, __builtin_amdgcn_raw_buffer_load_b128(vb, v_lane + (unsigned)(q_v_piece(D, 0, 16 * j) * 16), at, 0));
   };
 
   floatx4 o[J];
@@ -159,30 +165,32 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attn_qdecode_kernel(QAttnParam
     }
   };
 
-  // ---- the wavefront's blocks, every NW-th of the piece's: two in flight
-  int b = b_begin + w;
-  if (b < b_codes) {
-    Codes x, y;
-    load(x, b);
-#pragma unroll 1
-    while (true) {
-      const bool more = b + NW < b_codes;
-      load(y, more ? b + NW : b);
-      asm volatile("" ::: "memory");
-      block(x, b);
-      b += NW;
-      if (!more) break;
-      const bool again = b + NW < b_codes;
-      load(x, again ? b + NW : b);
-      asm volatile("" ::: "memory");
-      block(y, b);
-      b += NW;
-      if (!again) break;
-    }
-  }
-  if (b < b_end) {  // the rows that are not a whole block yet, in bf16
-    const int n = len - b * kQBlock;
+  // ---- the wavefront's blocks, every NW-th of the piece's, two in flight: in cyclic order from a place that differs from piece to piece and head to
+  // head, as pieces and heads lie powers of two apart, and workgroups in step would ask the same few memory channels for their rows
+  const int b_first = b_begin + w, n = b_first < b_codes ? (int)((unsigned)(b_codes - b_first + NW - 1) / (unsigned)NW) : 0, b_rest = b_first + NW * n;
+  auto next = [&](int b) __attribute__((always_inline)) -> int { return b + NW < b_rest ? b + NW : b_first; };
+  Codes x, y;
+  int b = b_first + NW * (int)(((((unsigned)(split * 8 + g) * 40503u) & 0xffffu) * (unsigned)n) >> 16), left = n;
+  if (n > 0) load(x, b, true);
+
+  // ---- The rows that are not a whole block, in bf16, are the wavefront's whose turn it is, the only one to read them: it also appends the new ones
+  if (b_rest == n_whole && n_whole < b_end) {
+    const int b = n_whole, n = len - b * kQBlock;
     const uint64_t slot = ((uint64_t)g * kQRing + (unsigned)b % kQRing) * BLOCK;
+    if (qp.k_new) {
+      const int64_t stride = (int64_t)p.n_kv_heads * D;
+      const __bf16 *k_new = qp.k_new + g * D, *v_new = qp.v_new + g * D;
+      unsigned short* v_slot = reinterpret_cast<unsigned short*>(qp.c.ring[1] + slot);
+      for (int i = l; i < C * (D / 8); i += 64) {
+        const int t = i / (D / 8), c = i % (D / 8), key = n - C + t;
+        const qbf16x8 k = finite_row(q_query<D>(k_new + t * stride, 8 * c, p.rope_cos ? p.rope_cos + t * (D / 2) : nullptr, p.rope_cos ? p.rope_sin + t * (D / 2) : nullptr));
+        const qbf16x8 v = finite_row(*reinterpret_cast<const qbf16x8*>(v_new + t * stride + 8 * c));
+        *reinterpret_cast<qbf16x8*>(qp.c.ring[0] + slot + q_k_piece(c >> 1, key) * 16 + (c & 1) * 8) = k;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v_slot[q_v_piece(D, q_key_group(key), 8 * c + e) * 16 + q_key_element(key)] = __builtin_bit_cast(unsigned short, (__bf16)v[e]);
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
     const unsigned char* kb = reinterpret_cast<const unsigned char*>(qp.c.ring[0] + slot) + 2 * k_lane;
     const unsigned char* vb = reinterpret_cast<const unsigned char*>(qp.c.ring[1] + slot) + 2 * v_lane;
     floatx4 s[4];
@@ -212,6 +220,21 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attn_qdecode_kernel(QAttnParam
     }
   }
 
+  if (n > 0) {
+#pragma unroll 1
+    while (true) {
+      const int b1 = next(b), b2 = next(b1);
+      load(y, b1, left > 1);
+      asm volatile("" ::: "memory");
+      block(x, b);
+      if (--left == 0) break;
+      load(x, b2, left > 1);
+      asm volatile("" ::: "memory");
+      block(y, b1);
+      if (--left == 0) break;
+      b = b2;
+    }
+  }
   // ---- the wavefronts' results meet in LDS: [wavefront][row][D] and [wavefront][row] (m, l)
   const float l_tot = pair_sum(row16_sum(l_run));
   if (c16 < rows) {

@@ -68,9 +68,10 @@ struct QLength {
 };
 
 int validate_qconfig(const kvfold_config_t* c);
-// Pieces that the keys of a step are cut into, and blocks of each; the kernel (decode: at most 16 packed rows a KV head).
+// Pieces that the keys of a step are cut into, and blocks of each; the kernel (decode: at most 16 packed rows a KV head); whether the
+// pieces meet in it.
 struct QPlan {
-  bool decode;
+  bool decode, meet;
   int units_per_wave, units_per_head, wgs_per_head, n_splits, blocks_per_split, n_wgs;
 };
 QPlan make_qplan(const kvfold_config_t& c, int n_cu, int64_t ws_rows, int n_tokens, int64_t len_after);
@@ -111,12 +112,24 @@ hipError_t launch_qread(const QReadParams& p, int head_dim, hipStream_t s);
 struct QAttnParams {
   AttnParams a;  // k_cache, v_cache: unused; tiles_per_split: blocks
   QRows c;
+  // The decoding kernel appends the chunk's rows itself, which fill no block (nullptr: the cache holds them already): as handed in, [C][Hkv][d]
+  const __bf16 *k_new, *v_new;
 };
 hipError_t launch_attn_qdecode(const QAttnParams& p, int head_dim, hipStream_t s);
 hipError_t launch_attn_q(const QAttnParams& p, int head_dim, int units_per_wave, hipStream_t s);
 
 typedef __attribute__((ext_vector_type(8))) __bf16 qbf16x8;
 typedef __attribute__((ext_vector_type(4))) unsigned quintx4;
+
+__device__ __forceinline__ unsigned finite_bf16(unsigned x) {
+  const unsigned m = x & 0x7fffu;
+  return m < 0x7f80u ? x : m == 0x7f80u ? (x & 0x8000u) | 0x7f7fu : 0u;
+}
+__device__ __forceinline__ qbf16x8 finite_row(qbf16x8 x) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = __builtin_bit_cast(__bf16, (unsigned short)finite_bf16(__builtin_bit_cast(unsigned short, (__bf16)x[e])));
+  return x;
+}
 
 // 16 codes as bf16, which holds them exactly: elements 0 .. 7 and 8 .. 15.  (Per pair two conversions that pick their byte, and a byte
 // permutation that takes the upper halves of both.)

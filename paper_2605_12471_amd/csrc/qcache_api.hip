@@ -225,13 +225,20 @@ int kvfold_qcache_step(kvfold_qcache_t* c, int layer, const void* q, const void*
   a.scale_log2e = c->scale * 1.4426950408889634f;
   a.rope_cos = rope_cos;
   a.rope_sin = rope_sin;
-  const bool meet = pl.decode && pl.n_splits > 1 && pl.n_splits <= kMeetSplits && c->meet_count;
+  const bool meet = pl.meet && c->meet_count;
   a.meet_count = meet ? c->meet_count : nullptr;
   finish_attn_params(a, pl.decode);
   p.c = c->rows(layer);
 
+  // The decoding kernel appends rows that fill no block itself, where its results lie apart from them: they are stored while other heads' rows are
+  // still read.
+  const size_t narrow = (size_t)n_tokens * f.n_kv_heads * f.head_dim * 2;
+  bool inside = pl.decode && len.len / kQBlock == (len.len + n_tokens) / kQBlock;
+  for (const void* rows : {k_new, v_new}) inside = inside && apart(rows, narrow, out, wide) && (!lse || apart(rows, narrow, lse, sums));
+  p.k_new = inside ? static_cast<const __bf16*>(k_new) : nullptr;
+  p.v_new = inside ? static_cast<const __bf16*>(v_new) : nullptr;
   const int64_t row = (int64_t)f.n_kv_heads * f.head_dim;
-  hipError_t e = append(c, layer, k_new, v_new, row, f.head_dim, n_tokens, rope_cos, rope_sin, s);
+  hipError_t e = inside ? hipSuccess : append(c, layer, k_new, v_new, row, f.head_dim, n_tokens, rope_cos, rope_sin, s);
   if (e != hipSuccess) return hip_fail(e);
   e = pl.decode ? launch_attn_qdecode(p, f.head_dim, s) : launch_attn_q(p, f.head_dim, pl.units_per_wave, s);
   if (e != hipSuccess) return hip_fail(e);

@@ -9,11 +9,6 @@ namespace kvfold {
 
 constexpr int kThreads = 256;
 
-__device__ __forceinline__ unsigned finite_bf16(unsigned x) {
-  const unsigned m = x & 0x7fffu;
-  return m < 0x7f80u ? x : m == 0x7f80u ? (x & 0x8000u) | 0x7f7fu : 0u;
-}
-
 // Elements of a piece as they come in (fresh: bit e, row of element e is one of the new ones), bf16 bits.
 template <int D, bool V>
 struct Piece {
