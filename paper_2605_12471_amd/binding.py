@@ -357,7 +357,7 @@ class KvFoldCache:
         # what every step needs, as plain Python values: fields of a ctypes structure are slow to read
         self._device, self._hq, self._hkv, self._d, self._capacity = device, n_q_heads, n_kv_heads, head_dim, capacity_tokens
         self._lib = load_library()
-        self._bound = False  # what the native step knows of this cache; None: there is none
+        self._bound = self._bound_weights = False  # what the native step, and the calls beside it, know of this cache; None: there is none
 
     def _bind(self):
         native, lib = _native_step(), self._lib
@@ -369,8 +369,18 @@ class KvFoldCache:
             self._bound = native.bind(*address, self.handle.value, self._device, self._hq, self._hkv, self._d, self.dtype_name != "f32")
         return self._bound
 
+    def _bind_weights(self):
+        native, lib = _native_step(), self._lib
+        if native is None or self.handle is None:
+            self._bound_weights = None
+        else:
+            address = [ctypes.cast(f, ctypes.c_void_p).value for f in (lib.kvfold_cache_weigh, lib.kvfold_cache_evict)]
+            self._bound_weights = native.bind_weights(*address, self.handle.value, self._device, self._hq, self._hkv, self._d, self._capacity,
+                                                      self.dtype_name != "f32")
+        return self._bound_weights
+
     def close(self):
-        self._bound = None
+        self._bound = self._bound_weights = None
         if getattr(self, "handle", None) is not None:
             rc = kvfold_cache_destroy(self.handle)
             self.handle = None
@@ -466,6 +476,15 @@ class KvFoldCache:
     def weigh(self, layer, q, lse, weights, add=True, rope=None, stream=None):
         """Enqueue kvfold_cache_weigh behind a step: its q [n][Hq][d] and the lse [Hq][n] that it left; weights fp32 [Hkv][capacity], added to or
         (add=False) set.  rope = (cos, sin), fp32 [n][d/2]: q is unrotated.  Returns weights."""
+        bound = self._bound_weights
+        if bound is False:
+            bound = self._bind_weights()
+        if bound is not None:
+            rc = _native.weigh(bound, layer, q, lse, weights, add, rope, stream)
+            if rc == 0:
+                return weights
+            if rc is not None:
+                raise KvFoldError(rc, "kvfold_cache_weigh")
         import torch
         f32, shape = torch.float32, q.shape
         n = shape[0] if len(shape) == 3 else -1
@@ -490,6 +509,25 @@ class KvFoldCache:
         is made, which takes the memory pool of torch's current stream: with `stream` given, hand in a workspace and kept of that stream."""
         import torch
         target = self if to is None else to
+        if target.handle is None:
+            raise ValueError("to: the cache is closed")
+        bound = self._bound_weights
+        if bound is False:
+            bound = self._bind_weights()
+        if bound is not None and to is not None:
+            into = to._bound_weights
+            if into is False:
+                into = to._bind_weights()
+        else:
+            into = None
+        if bound is not None and (to is None or into is not None) and type(n_keep) is int and 0 < n_keep and type(weights) is torch.Tensor:
+            rows = torch.empty((self._hkv, n_keep), dtype=torch.int32, device=weights.device) if kept is None else kept
+            space = torch.empty((max(kvfold_evict_workspace_bytes(self.handle, n_keep), 4),), dtype=torch.uint8, device=weights.device) if workspace is None else workspace
+            rc = _native.evict(bound, layer, weights, n_keep, n_sink, n_recent, into, to_layer, to_weights, rows, space, stream)
+            if rc == 0:
+                return rows
+            if rc is not None:
+                raise KvFoldError(rc, "kvfold_cache_evict")
         self._check("weights", weights, (self._hkv, self._capacity), torch.float32)
         if to_weights is not None:
             self._check("to_weights", to_weights, (self._hkv, target._capacity), torch.float32)
@@ -603,8 +641,19 @@ class KvFoldQuantCache:
             raise KvFoldError(rc, "kvfold_qcache_create")
         self._device, self._hq, self._hkv, self._d = device, n_q_heads, n_kv_heads, head_dim
         self._lib = load_library()
+        self._bound = False  # what the native calls know of this cache; None: there are none
+
+    def _bind(self):
+        native, lib = _native_step(), self._lib
+        if native is None or self.handle is None:
+            self._bound = None
+        else:
+            address = [ctypes.cast(f, ctypes.c_void_p).value for f in (lib.kvfold_qcache_step, lib.kvfold_qcache_read)]
+            self._bound = native.bind_quant(*address, self.handle.value, self._device, self._hq, self._hkv, self._d)
+        return self._bound
 
     def close(self):
+        self._bound = None
         if getattr(self, "handle", None) is not None:
             rc = kvfold_qcache_destroy(self.handle)
             self.handle = None
@@ -638,12 +687,22 @@ class KvFoldQuantCache:
     def step(self, layer, q, k_new, v_new, out, pos_offset=None, lse=None, stream=None, rope=None):
         """Enqueue one fold step: q, out [n][Hq][d], k_new, v_new [n][Hkv][d], lse fp32 [Hq][n], all contiguous.  rope = (cos, sin), fp32
         [n][d/2]: q and k_new are unrotated and the step rotates them."""
+        pos = self.length(layer) if pos_offset is None else pos_offset
+        bound = self._bound
+        if bound is False:
+            bound = self._bind()
+        if bound is not None:
+            rc = _native.quant_step(bound, layer, q, k_new, v_new, out, pos, lse, stream, rope)
+            if rc == 0:
+                return out
+            if rc is not None:
+                raise KvFoldError(rc, "kvfold_qcache_step")
         n = q.shape[0] if q.dim() == 3 else -1
         wide, narrow = (n, self._hq, self._d), (n, self._hkv, self._d)
         args = [_expect("q", q, self._bf16, self._device, wide), _expect("k_new", k_new, self._bf16, self._device, narrow),
                 _expect("v_new", v_new, self._bf16, self._device, narrow)]
         cos, sin = self._angles(rope, n)
-        rc = self._lib.kvfold_qcache_step(self.handle, layer, *args, n, self.length(layer) if pos_offset is None else pos_offset, cos, sin,
+        rc = self._lib.kvfold_qcache_step(self.handle, layer, *args, n, pos, cos, sin,
                                           _expect("out", out, self._bf16, self._device, wide),
                                           None if lse is None else _expect("lse", lse, self._f32, self._device, (self._hq, n)), self._stream(stream))
         if rc:
@@ -669,6 +728,15 @@ class KvFoldQuantCache:
         given = [t for t in (k_out, v_out) if t is not None]
         if not given:
             return
+        bound = self._bound
+        if bound is False:
+            bound = self._bind()
+        if bound is not None:
+            rc = _native.quant_read(bound, layer, first, k_out, v_out, stream)
+            if rc == 0:
+                return
+            if rc is not None:
+                raise KvFoldError(rc, "kvfold_qcache_read")
         n = given[0].shape[0] if given[0].dim() == 3 else -1
         ptr = [None if t is None else _expect(name, t, self._f32, self._device, (n, self._hkv, self._d)) for name, t in (("k_out", k_out), ("v_out", v_out))]
         rc = self._lib.kvfold_qcache_read(self.handle, layer, first, n, *ptr, self._stream(stream))
