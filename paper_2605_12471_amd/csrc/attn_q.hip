@@ -1,33 +1,38 @@
 // Chunk-prefix attention on a cache held in 8 bits, any number of rows.  A work unit is 32 consecutive packed (token, head of the group) rows
-// of a KV head, a wavefront owns U of them, a workgroup four wavefronts of one KV head and a piece of its blocks.
+// of a KV head, the work of one wavefront; a workgroup has NW of them of one KV head, eight where heads are 128 wide, and a piece of its blocks.
 //
-// Bound by the matrix instructions where rows are many.  A block of 64 keys is brought in as codes, half the bytes of bf16, a block
-// ahead, 64 bytes a thread (32 where heads are 64 wide); each thread widens its own to bf16, which holds them exactly, and puts them into LDS in the
-// order of the matrix instructions' operands, so that they are widened once for the workgroup's 128 U rows and every LDS access
-// is 16 bytes a lane, neighbours side by side.  V needs no transpose on the way: the layout (qcache.h) has its keys side by side.  Two
-// buffers, one barrier a block.
+// Bound by the matrix instructions and by issue.  A block of 64 keys is brought in as codes, half the bytes of bf16; each thread widens its own to
+// bf16, which holds them exactly, and puts them into LDS in the order of the matrix instructions' operands, so that they are widened once for
+// the workgroup's rows and every LDS access is 16 bytes a lane, neighbours side by side.  V needs no transpose on the way: the layout
+// (qcache.h) has its keys side by side.
 //
 // S^T = K Q^T and O^T = V^T P^T on the 32x32x16 shapes: a lane holds 32 logits of one query, whose weights are its operand of the second product
-// as they stand.  Scales, rounding points and the stale maximum as in the decoding kernel (attn_qdecode.hip).
+// as they stand.  Scales and rounding points as in the decoding kernel (attn_qdecode.hip).  The reference m of a row only has to keep the weights
+// inside the range of fp32.  It is the first block's maximum, and is not compared with another's while the row sees all of a block: the sum of a
+// block's weights, needed anyway, tells when it is far behind, and it follows by a power of two.  Logits that rise by more than fp32 holds
+// within one block lose the piece, which the workgroup then does again, with every block's maximum taken.
 #include "qcache.h"
 #include "wave_ops.h"
 
 namespace kvfold {
 
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 typedef __attribute__((ext_vector_type(4))) float floatx4;
 typedef __attribute__((ext_vector_type(2))) float floatx2;
 typedef __attribute__((ext_vector_type(16))) float floatx16;
 
-template <int D, int U>
-__global__ void __launch_bounds__(256, U == 1 ? 2 : 1) attn_q_kernel(QAttnParams qp) {
+template <int D, int NW>
+__global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
   const AttnParams& p = qp.a;
-  constexpr int KS = D / 16, JT = D / 32;    // contraction steps of S^T, tiles of O^T
-  constexpr int BLOCK = kQBlock * D;         // codes of a block
-  constexpr int T = BLOCK / 16 / 256;        // pieces of K, and of V, per thread
-  constexpr int KLDS = BLOCK * 2, BUF = 2 * KLDS;
-  constexpr float kStale = 16.0f;            // log2 units
-  __shared__ __attribute__((aligned(16))) unsigned char lds[2 * BUF];
+  constexpr int KS = D / 16, JT = D / 32;            // contraction steps of S^T, tiles of O^T
+  constexpr int BLOCK = kQBlock * D;                 // codes of a block
+  constexpr int NT = NW * 64, T = BLOCK / 16 / NT;   // threads; pieces of K, and of V, of each
+  constexpr int SLOT = BLOCK * 2;                    // bytes of a block's K, or V, in LDS
+  constexpr float kStale = 16.0f;                    // log2 units
+  constexpr float kFar = 0x1p60f, kLost = 0x1p100f;  // sums of a lane's weights in a block
+  static_assert(T * NT * 16 == BLOCK, "every thread has the same share of a block");
+  __shared__ __attribute__((aligned(16))) unsigned char lds[4 * SLOT];  // K, K, V, V
 
   const int lid = logical_workgroup(blockIdx.x, gridDim.x, p);
   if (lid >= p.n_wgs) return;
@@ -41,259 +46,334 @@ __global__ void __launch_bounds__(256, U == 1 ? 2 : 1) attn_q_kernel(QAttnParams
   const int C = p.n_tokens, Hq = p.n_q_heads, G = p.group, rows = C * G;
   const int len = (int)p.len_prev + C, n_whole = len / kQBlock;
 
-  // ---- the wavefront's rows
-  const int unit0 = (wg * 4 + w) * U;
-  int tok[U], row[U];
-  qbf16x8 qf[U][KS];
+  // ---- the wavefront's rows: lane (c32, h) holds columns 16 ks + 8 h .. + 7 of row c32
+  const int unit = wg * NW + w;
+  int my_vis;
+  qbf16x8 qf[KS];
+  {
+    const int r = unit * kRowsPerUnit + c32, row = r < rows ? r : rows - 1, tok = (int)quot((unsigned)row, p.by_group);
+    my_vis = (int)p.len_prev + tok + 1;
+    const __bf16* qrow = reinterpret_cast<const __bf16*>(p.q) + (uint64_t)(unsigned)(row + tok * (Hq - G) + g * G) * D;
+    const float* cs = p.rope_cos ? p.rope_cos + (int64_t)tok * (D / 2) : nullptr;
+    const float* sn = p.rope_cos ? p.rope_sin + (int64_t)tok * (D / 2) : nullptr;
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int r = (unit0 + u) * kRowsPerUnit + c32;
-    row[u] = r < rows ? r : rows - 1;
-    tok[u] = (int)quot((unsigned)row[u], p.by_group);
-    const __bf16* qrow = reinterpret_cast<const __bf16*>(p.q) + (uint64_t)(unsigned)(row[u] + tok[u] * (Hq - G) + g * G) * D;
-    const float* cs = p.rope_cos ? p.rope_cos + (int64_t)tok[u] * (D / 2) : nullptr;
-    const float* sn = p.rope_cos ? p.rope_sin + (int64_t)tok[u] * (D / 2) : nullptr;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[u][ks] = q_query<D>(qrow, 16 * ks + 8 * h, cs, sn);
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = q_query<D>(qrow, 16 * ks + 8 * h, cs, sn);
   }
   // Keys that the wavefront's first row sees, and its last one; that the workgroup's last row sees
   auto seen_by = [&](int r) __attribute__((always_inline)) -> int {
     r = r < rows ? r : rows - 1;
     return (int)p.len_prev + (int)quot((unsigned)r, p.by_group) + 1;
   };
-  const bool live = unit0 * kRowsPerUnit < rows;
-  const int vis_first = seen_by(unit0 * kRowsPerUnit), vis_last = live ? seen_by((unit0 + U) * kRowsPerUnit - 1) : 0;
-  const int vis_wg = seen_by((wg * 4 + 4) * U * kRowsPerUnit - 1);
-  const int b_begin = split * p.tiles_per_split;
-  int b_end = b_begin + p.tiles_per_split;
-  const int b_seen = (vis_wg + kQBlock - 1) / kQBlock;
-  if (b_end > b_seen) b_end = b_seen;
+  const int vis_first = seen_by(unit * kRowsPerUnit), vis_last = unit * kRowsPerUnit < rows ? seen_by((unit + 1) * kRowsPerUnit - 1) : 0;
+  const int vis_wg = seen_by((wg + 1) * NW * kRowsPerUnit - 1);
+  const int b_begin = split * p.tiles_per_split, b_seen = (vis_wg + kQBlock - 1) / kQBlock;
+  const int b_end = b_begin + p.tiles_per_split < b_seen ? b_begin + p.tiles_per_split : b_seen;
+  const int b_codes = b_end < n_whole ? b_end : n_whole;  // blocks before it are held as codes
 
-  const unsigned char* codes[2];
-  codes[0] = qp.c.codes[0] + (uint64_t)g * (uint64_t)qp.c.blocks * BLOCK;
-  codes[1] = qp.c.codes[1] + (uint64_t)g * (uint64_t)qp.c.blocks * BLOCK;
+  // ---- a block on its way: K fragment (tile t, step, half) at ((t KS + step) 2 + half) 512, V fragment (tile t, step, tile of O^T, half) at
+  // (((t 2 + step) JT + tile) 2 + half) 512, in two slots of each.  (By buffer accesses: a lane's place in a block is fixed and the
+  // block's is a scalar.  A head's codes take at most 2^31 bytes.)
+  __amdgpu_buffer_rsrc_t codes[2];
+#pragma unroll
+  for (int v = 0; v < 2; ++v)
+    codes[v] = __builtin_amdgcn_make_buffer_rsrc(qp.c.codes[v] + (uint64_t)g * (uint64_t)qp.c.blocks * BLOCK, 0, (unsigned)qp.c.blocks * (unsigned)BLOCK, 0x00020000);
   const float* scales = qp.c.scales + 2 * (uint64_t)g * (uint64_t)qp.c.blocks;
-
-  // ---- a block on its way: K fragment (tile t, step, half) at ((t KS + step) 2 + half) 512, V's (tile t, step, tile of O^T, half) behind them
   quintx4 raw[2][T];
-  auto load = [&](int b) __attribute__((always_inline)) {
+  auto load = [&](int v, int b) __attribute__((always_inline)) {
 #pragma unroll
-    for (int v = 0; v < 2; ++v)
-#pragma unroll
-      for (int j = 0; j < T; ++j) raw[v][j] = *reinterpret_cast<const quintx4*>(codes[v] + (uint64_t)(unsigned)b * BLOCK + (unsigned)(tid + 256 * j) * 16);
+    for (int j = 0; j < T; ++j)
+      raw[v][j] = __builtin_bit_cast(quintx4, __builtin_amdgcn_raw_buffer_load_b128(codes[v], (unsigned)tid * 16, (unsigned)b * (unsigned)BLOCK + (unsigned)(NT * j) * 16, 0));
   };
-  auto put = [&](unsigned char* buf, int v, int piece, const qbf16x8& lo, const qbf16x8& up) __attribute__((always_inline)) {
-    unsigned char* at;
-    int next;
+  auto put_half = [&](int v, int b, int piece, int half, const qbf16x8& x) __attribute__((always_inline)) {
+    unsigned char* at = lds + (2 * v + (b & 1)) * SLOT;
     if (v == 0) {
       const int c = piece >> 6, key = piece & 63;
-      at = buf + (((key >> 5) * KS + c) * 2 * 32 + (key & 31)) * 16;
-      next = 32 * 16;  // the other half
+      at += ((((key >> 5) * KS + c) * 2 + half) * 32 + (key & 31)) * 16;
     } else {
       const int kg = piece / D, col = piece % D;
-      at = buf + KLDS + ((((kg >> 1) * 2 * JT + (col >> 5)) * 2 + (kg & 1)) * 32 + (col & 31)) * 16;
-      next = JT * 2 * 32 * 16;  // the other step
+      at += (((((kg >> 1) * 2 + half) * JT + (col >> 5)) * 2 + (kg & 1)) * 32 + (col & 31)) * 16;
     }
-    *reinterpret_cast<qbf16x8*>(at) = lo;
-    *reinterpret_cast<qbf16x8*>(at + next) = up;
+    *reinterpret_cast<qbf16x8*>(at) = x;
   };
-  auto store = [&](unsigned char* buf) __attribute__((always_inline)) {
-#pragma unroll
-    for (int v = 0; v < 2; ++v)
-#pragma unroll
-      for (int j = 0; j < T; ++j) {
-        qbf16x8 lo, up;
-        q_widen(raw[v][j], lo, up);
-        put(buf, v, tid + 256 * j, lo, up);
-      }
+  // Asks for block b, and puts what was asked for into LDS, as far as there is such a block
+  auto load_any = [&](int v, int b) __attribute__((always_inline)) {
+    if (b < b_codes) load(v, b);
   };
-  // The rows that are not a whole block yet, in bf16; places without a row hold anything, in V they become 0 (0 times it has to be 0)
-  auto store_rest = [&](unsigned char* buf, int b) __attribute__((always_inline)) {
-    const int n = len - b * kQBlock;
-    const uint64_t slot = ((uint64_t)g * kQRing + (unsigned)b % kQRing) * BLOCK;
+  auto store_any = [&](int v, int b) __attribute__((always_inline)) {
+    int me = tid;
+    asm volatile("" : "+v"(me));  // (or what follows from it would be held in registers all the while)
+    if (b < b_codes) {
+#pragma unroll
+      for (int j = 0; j < T; ++j)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) put_half(v, b, me + NT * j, half, q_widen_half(raw[v][j], half));
+    } else if (b < b_end) {
+      // the rows that are not a whole block, in bf16; places without a row hold anything, in V they become 0 (0 times it has to be 0)
+      const int n = len - b * kQBlock;
+      const uint64_t slot = ((uint64_t)g * kQRing + (unsigned)b % kQRing) * BLOCK;
 #pragma unroll 1
-    for (int j = 0; j < T; ++j) {
-      const int piece = tid + 256 * j, kg = piece / D;
-      const qbf16x8* k = reinterpret_cast<const qbf16x8*>(qp.c.ring[0] + slot + piece * 16);
-      const qbf16x8* v = reinterpret_cast<const qbf16x8*>(qp.c.ring[1] + slot + piece * 16);
-      put(buf, 0, piece, k[0], k[1]);
-      qbf16x8 x[2] = {v[0], v[1]};
+      for (int j = 0; j < T; ++j) {
+        const int piece = me + NT * j, kg = piece / D;
+        const qbf16x8* at = reinterpret_cast<const qbf16x8*>(qp.c.ring[v] + slot + piece * 16);
+        qbf16x8 x[2] = {at[0], at[1]};
+        if (v == 1) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (32 * (kg >> 1) + 4 * (kg & 1) + 8 * (e >> 2) + (e & 3) >= n) x[e >> 3][e & 7] = (__bf16)0.f;
-      put(buf, 1, piece, x[0], x[1]);
+          for (int e = 0; e < 16; ++e)
+            if (32 * (kg >> 1) + 4 * (kg & 1) + 8 * (e >> 2) + (e & 3) >= n) x[e >> 3][e & 7] = (__bf16)0.f;
+        }
+        put_half(v, b, piece, 0, x[0]);
+        put_half(v, b, piece, 1, x[1]);
+      }
     }
   };
 
-  floatx16 o[U][JT];
-  float m_run[U], l_run[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    m_run[u] = -INFINITY;
-    l_run[u] = 0.f;
+  floatx16 o[JT];
+  float m_run, l_run;
+  auto clear = [&]() __attribute__((always_inline)) {
+    m_run = -INFINITY;
+    l_run = 0.f;
 #pragma unroll
     for (int j = 0; j < JT; ++j)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[u][j][i] = 0.f;
-  }
+      for (int i = 0; i < 16; ++i) o[j][i] = 0.f;
+  };
+  clear();
 
-  auto attend = [&](const unsigned char* buf, int b, float k_scale, float v_scale) __attribute__((always_inline)) {
-    floatx16 s[U][2];
+  constexpr floatx16 zero = {};
+  // S^T of a block
+  auto logits = [&](floatx16 (&s)[2], int b) __attribute__((always_inline)) {
+    const unsigned char* buf = lds + (b & 1) * SLOT + l * 16;
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int ks = 0; ks < KS; ++ks) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[u][t][i] = 0.f;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const qbf16x8 k = *reinterpret_cast<const qbf16x8*>(buf + ((t * KS + ks) * 64 + l) * 16);
-#pragma unroll
-        for (int u = 0; u < U; ++u) s[u][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qf[u][ks], s[u][t], 0, 0, 0);
-      }
+        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const qbf16x8*>(buf + (t * KS + ks) * 1024), qf[ks], ks == 0 ? zero : s[t], 0, 0, 0);
+      if (ks % 2) __builtin_amdgcn_sched_barrier(0);  // (four operands on their way at a time, for want of registers)
+    }
+  };
+  // The reference, before a block's exponentials: masks S^T, and moves rows whose maximum asks for it.  Only these move, so that a row's arithmetic never
+  // depends on its wave neighbours.
+  auto reference = [&](floatx16 (&s)[2], int b, float to_log2) __attribute__((always_inline)) {
     const int key0 = b * kQBlock;
     if (key0 + kQBlock > vis_first) {  // wave-uniform: some row does not see the whole block
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int rel = (int)p.len_prev + tok[u] + 1 - key0 - 4 * h;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (32 * t + 8 * (i >> 2) + (i & 3) >= rel) s[u][t][i] = -INFINITY;
-      }
-    }
-    const float to_log2 = q_to_log2(k_scale, p.scale_log2e);
-    float mx[U];
-    bool mine[U], any = false;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      mx[u] = -INFINITY;
+      const int rel = my_vis - key0 - 4 * h;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) mx[u] = fmaxf(mx[u], s[u][t][i]);
-      mx[u] = pair_max(mx[u]);
-      mx[u] *= to_log2;
-      mine[u] = mx[u] > m_run[u] + kStale || (m_run[u] == -INFINITY && mx[u] > -INFINITY);
-      any |= mine[u];
+        for (int i = 0; i < 16; ++i)
+          if (32 * t + 8 * (i >> 2) + (i & 3) >= rel) s[t][i] = -INFINITY;
     }
-    if (__any(any)) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const float m2 = mine[u] ? mx[u] : m_run[u];
-        const float alpha = m_run[u] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[u] - m2);
-        m_run[u] = m2;
-        l_run[u] *= alpha;
-#pragma unroll
-        for (int j = 0; j < JT; ++j)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[u][j][i] *= alpha;
-      }
-    }
-    qbf16x8 pf[U][2][2];
-    const float log2_v = __builtin_amdgcn_logf(v_scale), inv_v = __builtin_amdgcn_rcpf(v_scale);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const float ref = (m_run[u] == -INFINITY ? 0.f : m_run[u]) - log2_v;
-      float sum = 0.f;
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][t][i], to_log2, -ref));
-          sum += a;
-          pf[u][t][i >> 3][i & 7] = (__bf16)a;
-        }
-      l_run[u] = __builtin_fmaf(sum, inv_v, l_run[u]);
-    }
+    float mx = -INFINITY;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int st = 0; st < 2; ++st)
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[t][i]);
+    mx = pair_max(mx) * to_log2;
+    const bool mine = mx > m_run + kStale || (m_run == -INFINITY && mx > -INFINITY);
+    if (__any(mine)) {
+      const float m2 = mine ? mx : m_run;
+      const float alpha = m_run == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m2);  // (without history: l = 0, O = 0)
+      m_run = m2;
+      l_run *= alpha;
 #pragma unroll
-        for (int j = 0; j < JT; ++j) {
-          const qbf16x8 v = *reinterpret_cast<const qbf16x8*>(buf + KLDS + (((t * 2 + st) * JT + j) * 64 + l) * 16);
+      for (int j = 0; j < JT; ++j)
 #pragma unroll
-          for (int u = 0; u < U; ++u) o[u][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[u][t][st], o[u][j], 0, 0, 0);
+        for (int i = 0; i < 16; ++i) o[j][i] *= alpha;
+    }
+  };
+  // A block's exponentials and outputs, one after the other
+  auto attend = [&](const floatx16 (&s)[2], int b, float to_log2, float v_scale) __attribute__((always_inline)) {
+    const float ref = (m_run == -INFINITY ? 0.f : m_run) - __builtin_amdgcn_logf(v_scale);
+    qbf16x8 pf[2][2];
+    float sum = 0.f;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], to_log2, -ref));
+        sum += a;
+        pf[t][i >> 3][i & 7] = (__bf16)a;
+      }
+    l_run = __builtin_fmaf(sum, __builtin_amdgcn_rcpf(v_scale), l_run);
+    const unsigned char* buf = lds + (2 + (b & 1)) * SLOT + l * 16;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+#pragma unroll
+        for (int j = 0; j < JT; ++j)
+          o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const qbf16x8*>(buf + ((t * 2 + st) * JT + j) * 1024), pf[t][st], o[j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+  };
+  // The same, laid out by hand, with S^T of the next block: 2 KS slots with a matrix instruction of S^T, 4 JT with one of O^T.  Behind each stands
+  // an even share of what else there is to do: this block's exponentials, done by the time that O^T asks for them (after 7/8 of the slots), and the
+  // codes of K of block b + 2 and V of block b + 1 that go into LDS.  Operands are read kAhead slots ahead.
+  bool lost = false;
+  auto turn = [&](const floatx16 (&s)[2], floatx16 (&x)[2], int b, float to_log2, float v_scale) __attribute__((always_inline)) {
+    constexpr int SM = 2 * KS, OM = 4 * JT, NS = SM + OM, kAhead = 2;
+    constexpr int WORDS = 2 * T * 8, E = NS - NS / 8;  // words of widened codes; slots with exponentials
+    const unsigned char *kbuf = lds + ((b + 1) & 1) * SLOT + l * 16, *vbuf = lds + (2 + (b & 1)) * SLOT + l * 16;
+    auto operand = [&](int i) __attribute__((always_inline)) -> qbf16x8 {  // of slot i
+      return *reinterpret_cast<const qbf16x8*>(i < SM ? kbuf + ((i & 1) * KS + (i >> 1)) * 1024 : vbuf + (i - SM) * 1024);
+    };
+    qbf16x8 f[kAhead + 1];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) f[i] = operand(i);
+    const float inv_v = __builtin_amdgcn_rcpf(v_scale), ref = (m_run == -INFINITY ? 0.f : m_run) - __builtin_amdgcn_logf(v_scale);
+    float sum = 0.f, last = 0.f;
+    quintx4 pb[2][2], wide;
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      if (i + kAhead < NS) f[(i + kAhead) % (kAhead + 1)] = operand(i + kAhead);
+      const qbf16x8 a = f[i % (kAhead + 1)];
+      const int j = i - SM;
+      if (i < SM)
+        x[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[i >> 1], i < 2 ? zero : x[i & 1], 0, 0, 0);
+      else
+        o[j % JT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(qbf16x8, pb[j / JT / 2][j / JT % 2]), o[j % JT], 0, 0, 0);
+      if (i < E) {
+#pragma unroll
+        for (int e = 32 * i / E; e < 32 * (i + 1) / E; ++e) {
+          const float weight = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 4][e & 15], to_log2, -ref));
+          sum += weight;
+          if (e & 1) {
+            bf16x2 pk;
+            pk[0] = (__bf16)last;
+            pk[1] = (__bf16)weight;
+            pb[e >> 4][e >> 3 & 1][e >> 1 & 3] = __builtin_bit_cast(unsigned, pk);
+          }
+          last = weight;
         }
+      }
+#pragma unroll
+      for (int k = WORDS * i / NS; k < WORDS * (i + 1) / NS; ++k) {
+        const int v = k / (8 * T), piece = k / 8 % T;
+        wide[k % 4] = q_widen_word(raw[v][piece], k % 8);
+        if (k % 4 == 3) put_half(v, b + 2 - v, tid + NT * piece, k / 4 % 2, __builtin_bit_cast(qbf16x8, wide));
+      }
+      if (i == NS / 2) load(0, b + 3);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    load(1, b + 2);
+    l_run = __builtin_fmaf(sum, inv_v, l_run);
+    if (__builtin_expect(__any(!(sum * inv_v < kFar)), 0)) {
+      // Logits far above their row's reference: it follows by a power of two.  Beyond what fp32 holds all is to be done again.
+      const float top = pair_max(sum * inv_v);
+      lost |= !(pair_sum(sum * inv_v) < kLost);
+      const int by = top >= kFar && top < kLost ? __builtin_amdgcn_frexp_expf(top) : 0;
+      const float alpha = __builtin_amdgcn_ldexpf(1.f, -by);
+      m_run += (float)by;
+      l_run *= alpha;
+#pragma unroll
+      for (int jj = 0; jj < JT; ++jj)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[jj][i] *= alpha;
+    }
   };
 
-  if (b_begin < b_end) {
-    int at = 0;
-    floatx2 scale = {1.f, 1.f}, next = {1.f, 1.f};
-    if (b_begin < n_whole) {
-      load(b_begin);
-      scale = *reinterpret_cast<const floatx2*>(scales + 2 * (unsigned)b_begin);
-      store(lds);
-    } else {
-      store_rest(lds, b_begin);
-    }
+  // (Waited for here: in the loop the compiler would wait for the block that has just been asked for.)
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
+  floatx16 s[2], x[2];
+  floatx2 scale;
+  auto step = [&](floatx16 (&now)[2], floatx16 (&next)[2], int b) __attribute__((always_inline)) {
+    const floatx2 scale_next = *reinterpret_cast<const floatx2*>(scales + 2 * (unsigned)(b + 1));
+    const float to_log2 = q_to_log2(scale.x, p.scale_log2e);
+    // every row sees all of the block, and has a reference
+    if (!__all(b * kQBlock + kQBlock <= vis_first && m_run != -INFINITY)) reference(now, b, to_log2);
+    turn(now, next, b, to_log2, scale.y);
+    scale = scale_next;
     __syncthreads();
+  };
+  auto scale_of = [&](int b) __attribute__((always_inline)) -> floatx2 {
+    return b < b_codes ? *reinterpret_cast<const floatx2*>(scales + 2 * (unsigned)b) : floatx2{1.f, 1.f};
+  };
 #pragma unroll 1
-    for (int b = b_begin; b < b_end; ++b) {
-      const bool more = b + 1 < b_end, more_codes = more && b + 1 < n_whole;
-      if (more_codes) {
-        load(b + 1);
-        next = *reinterpret_cast<const floatx2*>(scales + 2 * (unsigned)(b + 1));
+  for (bool again = false; b_begin < b_end; again = true) {  // the second time, if there is one, with every block's maximum
+    load_any(0, b_begin);
+    load_any(1, b_begin);
+    store_any(0, b_begin);
+    store_any(1, b_begin);
+    load_any(0, b_begin + 1);
+    store_any(0, b_begin + 1);
+    load_any(0, b_begin + 2);
+    load_any(1, b_begin + 1);
+    scale = scale_of(b_begin);
+    __syncthreads();
+    logits(s, b_begin);
+    __syncthreads();  // (K of block b_begin + 2 is going to take its place)
+    int b = b_begin;
+#pragma unroll 1
+    for (; !again && b + 4 < b_codes; b += 2) {
+      step(s, x, b);
+      step(x, s, b + 1);
+    }
+#pragma unroll 1
+    for (; b < b_end; ++b) {
+      store_any(0, b + 2);
+      store_any(1, b + 1);
+      load_any(0, b + 3);
+      load_any(1, b + 2);
+      if (b * kQBlock < vis_last) {
+        const float to_log2 = q_to_log2(scale.x, p.scale_log2e);
+        reference(s, b, to_log2);
+        attend(s, b, to_log2, scale.y);
+        if (b + 1 < b_end) logits(s, b + 1);
       }
-      if (b * kQBlock < vis_last) attend(lds + at, b, scale.x, scale.y);
-      if (more_codes) {
-        store(lds + (at ^ BUF));
-        scale = next;
-      } else if (more) {
-        store_rest(lds + (at ^ BUF), b + 1);
-        scale = floatx2{1.f, 1.f};
-      }
-      at ^= BUF;
+      scale = scale_of(b + 1);
       __syncthreads();
     }
+    if (again) break;
+    int* flag = reinterpret_cast<int*>(lds);  // (behind the last barrier)
+    if (tid == 0) *flag = 0;
+    __syncthreads();
+    if (lost) *flag = 1;
+    __syncthreads();
+    const int redo = *flag;
+    __syncthreads();
+    if (!redo) break;
+    clear();
   }
 
   // ---- out, or what the piece leaves for the merge
-  const int64_t n_rows = (int64_t)C * Hq;
+  const float l_tot = pair_sum(l_run);
+  int lane = threadIdx.x;
+  asm volatile("" : "+v"(lane));  // (found again, not held through the loop)
+  const int half = lane >> 5 & 1, r = unit * kRowsPerUnit + (lane & 31);
+  if (r >= rows) return;
+  const int t = (int)quot((unsigned)r, p.by_group), head = g * G + r - t * G;
+  const int64_t at = (int64_t)t * Hq + head;
+  if (p.n_splits == 1) {
+    const float inv = 1.f / l_tot;
+    __bf16* out = reinterpret_cast<__bf16*>(p.out) + at * D + 4 * half;
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const float l_tot = pair_sum(l_run[u]);
-    if ((unit0 + u) * kRowsPerUnit + c32 >= rows) continue;
-    const int head = g * G + row[u] - tok[u] * G;
-    const int64_t at = (int64_t)tok[u] * Hq + head;
-    if (p.n_splits == 1) {
-      const float inv = 1.f / l_tot;
-      __bf16* out = reinterpret_cast<__bf16*>(p.out) + at * D + 4 * h;
+    for (int j = 0; j < JT; ++j)
 #pragma unroll
-      for (int j = 0; j < JT; ++j)
+      for (int i = 0; i < 16; i += 4) {
+        bf16x4 v;
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-          bf16x4 v;
+        for (int e = 0; e < 4; ++e) v[e] = (__bf16)(o[j][i + e] * inv);
+        *reinterpret_cast<bf16x4*>(out + 32 * j + 2 * i) = v;
+      }
+    if (p.lse && half == 0) p.lse[(int64_t)head * C + t] = (m_run + __builtin_amdgcn_logf(l_tot)) * 0.6931471805599453f;
+  } else {
+    const int64_t piece = (int64_t)split * C * Hq + at;
+    float* out = p.part_o + piece * D + 4 * half;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = (__bf16)(o[u][j][i + e] * inv);
-          *reinterpret_cast<bf16x4*>(out + 32 * j + 2 * i) = v;
-        }
-      if (p.lse && h == 0) p.lse[(int64_t)head * C + tok[u]] = (m_run[u] + __builtin_amdgcn_logf(l_tot)) * 0.6931471805599453f;
-    } else {
-      float* out = p.part_o + ((int64_t)split * n_rows + at) * D + 4 * h;
+    for (int j = 0; j < JT; ++j)
 #pragma unroll
-      for (int j = 0; j < JT; ++j)
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) *reinterpret_cast<floatx4*>(out + 32 * j + 2 * i) = floatx4{o[u][j][i], o[u][j][i + 1], o[u][j][i + 2], o[u][j][i + 3]};
-      if (h == 0) *reinterpret_cast<floatx2*>(p.part_ml + ((int64_t)split * n_rows + at) * 2) = floatx2{m_run[u], l_tot};
-    }
+      for (int i = 0; i < 16; i += 4) *reinterpret_cast<floatx4*>(out + 32 * j + 2 * i) = floatx4{o[j][i], o[j][i + 1], o[j][i + 2], o[j][i + 3]};
+    if (half == 0) *reinterpret_cast<floatx2*>(p.part_ml + piece * 2) = floatx2{m_run, l_tot};
   }
 }
 
-hipError_t launch_attn_q(const QAttnParams& p, int head_dim, int units_per_wave, hipStream_t s) {
-  const dim3 grid(padded_grid(p.a.n_wgs)), block(256);
-  if (head_dim == 128 && units_per_wave == 2)
-    hipLaunchKernelGGL((attn_q_kernel<128, 2>), grid, block, 0, s, p);
-  else if (head_dim == 128)
-    hipLaunchKernelGGL((attn_q_kernel<128, 1>), grid, block, 0, s, p);
-  else if (units_per_wave == 2)
-    hipLaunchKernelGGL((attn_q_kernel<64, 2>), grid, block, 0, s, p);
+hipError_t launch_attn_q(const QAttnParams& p, int head_dim, hipStream_t s) {
+  const dim3 grid(padded_grid(p.a.n_wgs));
+  if (head_dim == 128)
+    hipLaunchKernelGGL((attn_q_kernel<128, 8>), grid, dim3(512), 0, s, p);
   else
-    hipLaunchKernelGGL((attn_q_kernel<64, 1>), grid, block, 0, s, p);
+    hipLaunchKernelGGL((attn_q_kernel<64, 4>), grid, dim3(256), 0, s, p);
   return hipGetLastError();
 }
 

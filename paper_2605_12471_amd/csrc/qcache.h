@@ -72,7 +72,7 @@ int validate_qconfig(const kvfold_config_t* c);
 // pieces meet in it.
 struct QPlan {
   bool decode, meet;
-  int units_per_wave, units_per_head, wgs_per_head, n_splits, blocks_per_split, n_wgs;
+  int waves_per_wg, units_per_head, wgs_per_head, n_splits, blocks_per_split, n_wgs;  // a wavefront has a unit of 32 rows
 };
 QPlan make_qplan(const kvfold_config_t& c, int n_cu, int64_t ws_rows, int n_tokens, int64_t len_after);
 
@@ -116,7 +116,7 @@ struct QAttnParams {
   const __bf16 *k_new, *v_new;
 };
 hipError_t launch_attn_qdecode(const QAttnParams& p, int head_dim, hipStream_t s);
-hipError_t launch_attn_q(const QAttnParams& p, int head_dim, int units_per_wave, hipStream_t s);
+hipError_t launch_attn_q(const QAttnParams& p, int head_dim, hipStream_t s);
 
 typedef __attribute__((ext_vector_type(8))) __bf16 qbf16x8;
 typedef __attribute__((ext_vector_type(4))) unsigned quintx4;
@@ -131,20 +131,21 @@ __device__ __forceinline__ qbf16x8 finite_row(qbf16x8 x) {
   return x;
 }
 
-// 16 codes as bf16, which holds them exactly: elements 0 .. 7 and 8 .. 15.  (Per pair two conversions that pick their byte, and a byte
-// permutation that takes the upper halves of both.)
-__device__ __forceinline__ void q_widen(const quintx4& codes, qbf16x8& lo, qbf16x8& up) {
-  quintx4 r[2];
+// Two of 16 codes as bf16, which holds them exactly: two conversions that pick their byte, and a byte permutation that takes the upper halves of both.
+__device__ __forceinline__ unsigned q_widen_word(const quintx4& codes, int w) {
+  const unsigned x = codes[w >> 1];
+  const float f0 = (float)(int)(signed char)(x >> (w & 1 ? 16 : 0)), f1 = (float)(int)(signed char)(x >> (w & 1 ? 24 : 8));
+  return __builtin_amdgcn_perm(__float_as_uint(f1), __float_as_uint(f0), 0x07060302u);
+}
+__device__ __forceinline__ qbf16x8 q_widen_half(const quintx4& codes, int half) {
+  quintx4 r;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const unsigned x = codes[w];
-    const float f0 = (float)(int)(signed char)(x), f1 = (float)(int)(signed char)(x >> 8);
-    const float f2 = (float)(int)(signed char)(x >> 16), f3 = (float)(int)(signed char)(x >> 24);
-    r[w >> 1][2 * (w & 1)] = __builtin_amdgcn_perm(__float_as_uint(f1), __float_as_uint(f0), 0x07060302u);
-    r[w >> 1][2 * (w & 1) + 1] = __builtin_amdgcn_perm(__float_as_uint(f3), __float_as_uint(f2), 0x07060302u);
-  }
-  lo = __builtin_bit_cast(qbf16x8, r[0]);
-  up = __builtin_bit_cast(qbf16x8, r[1]);
+  for (int w = 0; w < 4; ++w) r[w] = q_widen_word(codes, 4 * half + w);
+  return __builtin_bit_cast(qbf16x8, r);
+}
+__device__ __forceinline__ void q_widen(const quintx4& codes, qbf16x8& lo, qbf16x8& up) {
+  lo = q_widen_half(codes, 0);
+  up = q_widen_half(codes, 1);
 }
 
 // What a block's logits are multiplied by; above 0, so that a masked logit, -inf, stays that.

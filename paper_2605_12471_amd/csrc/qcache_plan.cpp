@@ -29,10 +29,10 @@ QPlan make_qplan(const kvfold_config_t& c, int n_cu, int64_t ws_rows, int n_toke
   QPlan pl{};
   pl.decode = rows <= 16;
   pl.units_per_head = units_of_head(n_tokens, G);
-  pl.units_per_wave = 1;
-  pl.wgs_per_head = pl.decode ? 1 : (pl.units_per_head + kUnitsPerWg * pl.units_per_wave - 1) / (kUnitsPerWg * pl.units_per_wave);
+  pl.waves_per_wg = c.head_dim == 128 ? 8 : 4;
+  pl.wgs_per_head = pl.decode ? 1 : (pl.units_per_head + pl.waves_per_wg - 1) / pl.waves_per_wg;
   const int64_t per_split = (int64_t)c.n_kv_heads * pl.wgs_per_head;
-  int64_t splits = pl.decode ? decode_splits(blocks, std::min<int64_t>(std::max<int64_t>(1, n_cu / c.n_kv_heads), kMaxSplits)) : std::min<int64_t>(2 * (int64_t)n_cu / per_split, blocks);
+  int64_t splits = pl.decode ? decode_splits(blocks, std::min<int64_t>(std::max<int64_t>(1, n_cu / c.n_kv_heads), kMaxSplits)) : std::min<int64_t>((c.head_dim == 128 ? 1 : 2) * (int64_t)n_cu / per_split, blocks);
   splits = std::min<int64_t>(splits, kMaxSplits);
   splits = std::min(splits, ws_rows / ((int64_t)n_tokens * c.n_q_heads));
   splits = std::max<int64_t>(splits, 1);

@@ -122,7 +122,7 @@ static void plans() {
     CHECK((int64_t)(p.n_splits - 1) * p.blocks_per_split < blocks && (int64_t)p.n_splits * p.blocks_per_split >= blocks);  // no piece without a block
     CHECK(p.n_splits == 1 || (int64_t)p.n_splits * n * hq <= ws);
     CHECK(p.n_wgs == hkv * p.wgs_per_head * p.n_splits);
-    CHECK(p.decode ? n * (hq / hkv) <= 16 && p.wgs_per_head == 1 : p.wgs_per_head * kUnitsPerWg * p.units_per_wave >= p.units_per_head);
+    CHECK(p.decode ? n * (hq / hkv) <= 16 && p.wgs_per_head == 1 : p.wgs_per_head * p.waves_per_wg >= p.units_per_head && (p.wgs_per_head - 1) * p.waves_per_wg < p.units_per_head);
     const QLayout l = q_layout(c);
     CHECK(l.blocks * kQBlock >= capacity && l.codes % 256 == 0 && l.scales % 256 == 0 && l.ring % 256 == 0);
     CHECK(l.layer == 2 * l.codes + l.scales + 2 * l.ring);

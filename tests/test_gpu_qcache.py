@@ -192,6 +192,24 @@ def test_logits_that_jump(profile, n):
         f.step(m, data=(q, k, v))
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("profile", [lambda j: 45.0 * (j >= 500), lambda j: 60.0 * (j >= 1100), lambda j: 100.0 * ((j >= 300) + (j >= 900)), lambda j: 0.4 * j,
+                                     lambda j: 90.0 * (j == 700), lambda j: -200.0 * (j < 130), lambda j: 80.0 * (j >= 1550)])
+def test_logits_that_jump_far_behind_a_piece_s_first_block(d, profile):
+    """Jumps of 2^65 and more between blocks of a piece (many rows, so that pieces are long): the reference follows, or the piece is done again."""
+    hq, hkv, prev, n = 16, 8, 1400, 1000
+    f = Fold(hq, hkv, d, prev + n)
+    g = torch.Generator().manual_seed(d)
+    u = torch.nn.functional.normalize(torch.randn(d, generator=g), dim=0)
+    level = torch.tensor([float(profile(j)) for j in range(prev + n)])
+    k = (0.1 * torch.randn((prev + n, hkv, d), generator=g) + 0.5 * level[:, None, None] * u).to(torch.bfloat16)
+    v = torch.randn((prev + n, hkv, d), generator=g).to(torch.bfloat16)
+    q = (0.1 * torch.randn((n, hq, d), generator=g) + 2 * math.sqrt(d) * u).to(torch.bfloat16)
+    f.cache.append(0, k[:prev].cuda(), v[:prev].cuda())
+    f.joined(k[:prev], v[:prev])
+    f.step(n, data=(q, k[prev:], v[prev:]))
+
+
 def test_rewinding():
     f = Fold(8, 2, 128, 1000)
     f.append(500)
