@@ -38,9 +38,9 @@ __device__ __forceinline__ void give(const WeighParams& p, int g, int key, float
   *at = p.add ? *at + w : w;
 }
 
-// Many rows, bf16.  A workgroup has 32 KB KW keys of one KV head, a wavefront 32 KB of them and, of the UB RW units that are in LDS at a time, every RW-th: RW
+// Many rows, bf16.  A workgroup has 32 KW keys of one KV head, a wavefront 32 of them and, of the UB RW units that are in LDS at a time, every RW-th: RW
 // wavefronts share keys where there are too few keys for the chip, and add up what they have in the end.
-template <int D, int KB, int KW, int RW, int UB>
+template <int D, int KW, int RW, int UB>
 __global__ void __launch_bounds__(64 * KW * RW, 2) weigh_bf16_kernel(WeighParams p) {
   constexpr int KS = D / 16, CH = D / 8, NT = 64 * KW * RW, STAGE = RW * UB, T = STAGE * 32 * CH / NT, ROW = D * 2 + 16, UNIT = 32 * ROW;
   __shared__ __attribute__((aligned(16))) unsigned char q_lds[2 * STAGE * UNIT];
@@ -48,18 +48,13 @@ __global__ void __launch_bounds__(64 * KW * RW, 2) weigh_bf16_kernel(WeighParams
   static_assert(STAGE * 32 <= NT && T * NT == STAGE * 32 * CH, "a thread has the same share of every stage");
   const int tid = threadIdx.x, l = tid & 63, h = l >> 5, c32 = l & 31, w = __builtin_amdgcn_readfirstlane(tid >> 6), kw = w % KW, rw = w / KW;
   const int g = blockIdx.y, rows = p.n_tokens * p.group, units = (rows + 31) / 32, prev = p.len - p.n_tokens;
-  const int wg_key = blockIdx.x * (KW * 32 * KB), key0 = wg_key + kw * (32 * KB);
+  const int wg_key = blockIdx.x * (KW * 32), key0 = wg_key + kw * 32, key = key0 + c32;
 
   // ---- the keys: lane (key, h) holds columns 16 ks + 8 h .. + 7
   const __bf16* k_head = reinterpret_cast<const __bf16*>(p.k) + (int64_t)g * p.capacity * D;
-  qbf16x8 kf[KB][KS];
+  qbf16x8 kf[KS];
 #pragma unroll
-  for (int b = 0; b < KB; ++b) {
-    int key = key0 + 32 * b + c32;
-    if (key >= p.len) key = p.len - 1;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) kf[b][ks] = *reinterpret_cast<const qbf16x8*>(k_head + (int64_t)key * D + 16 * ks + 8 * h);
-  }
+  for (int ks = 0; ks < KS; ++ks) kf[ks] = *reinterpret_cast<const qbf16x8*>(k_head + (int64_t)(key < p.len ? key : p.len - 1) * D + 16 * ks + 8 * h);
 
   // ---- a stage on its way: its rows, ROW bytes apart (no two of sixteen in the same banks), and what the logits' sums begin with
   qbf16x8 q_in[T];
@@ -89,12 +84,10 @@ __global__ void __launch_bounds__(64 * KW * RW, 2) weigh_bf16_kernel(WeighParams
 
   // The first unit with a row that sees the workgroup's first key: row i of the chunk sees keys up to prev + i
   const int first_tok = wg_key > prev ? wg_key - prev : 0, u_begin = (int)((int64_t)first_tok * p.group / 32);
-  float sum[KB];
-#pragma unroll
-  for (int b = 0; b < KB; ++b) sum[b] = 0.f;
+  float sum = 0.f;
   // S - lse of a unit, in units of the logits before their scale; -inf where a row does not see the key
-  floatx16 s[KB];
-  auto logits = [&](int slot, floatx16 (&x)[KB]) __attribute__((always_inline)) {
+  floatx16 s;
+  auto logits = [&](int slot, floatx16& x) __attribute__((always_inline)) {
     floatx16 from;
 #pragma unroll
     for (int i = 0; i < 16; i += 4) {
@@ -105,26 +98,20 @@ __global__ void __launch_bounds__(64 * KW * RW, 2) weigh_bf16_kernel(WeighParams
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       const qbf16x8 q = *reinterpret_cast<const qbf16x8*>(q_lds + slot * UNIT + c32 * ROW + h * 16 + ks * 32);
-#pragma unroll
-      for (int b = 0; b < KB; ++b) x[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, kf[b][ks], ks == 0 ? from : x[b], 0, 0, 0);
+      x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, kf[ks], ks == 0 ? from : x, 0, 0, 0);
     }
   };
   auto mask = [&](int u) __attribute__((always_inline)) {
-    if (prev + (int)quot((unsigned)(u * 32), p.by_group) < key0 + 32 * KB - 1) {  // some row does not see all of the wavefront's keys
+    if (prev + (int)quot((unsigned)(u * 32), p.by_group) < key0 + 31) {  // some row does not see all of the wavefront's keys
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const int at = prev + (int)quot((unsigned)(u * 32 + 8 * (i >> 2) + 4 * h + (i & 3)), p.by_group);
-#pragma unroll
-        for (int b = 0; b < KB; ++b)
-          if (key0 + 32 * b + c32 > at) s[b][i] = -INFINITY;
+        if (key > prev + (int)quot((unsigned)(u * 32 + 8 * (i >> 2) + 4 * h + (i & 3)), p.by_group)) s[i] = -INFINITY;
       }
     }
   };
   auto add_up = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-#pragma unroll
-      for (int b = 0; b < KB; ++b) sum[b] += __builtin_amdgcn_exp2f(s[b][i] * p.scale_log2e);
+    for (int i = 0; i < 16; ++i) sum += __builtin_amdgcn_exp2f(s[i] * p.scale_log2e);
   };
   // A unit's exponentials stand among the next one's matrix instructions
   load(u_begin);
@@ -143,11 +130,10 @@ __global__ void __launch_bounds__(64 * KW * RW, 2) weigh_bf16_kernel(WeighParams
         logits(buf * STAGE + i * RW + rw, s);
       } else {
         mask(u_last);
-        floatx16 x[KB];
+        floatx16 x;
         logits(buf * STAGE + i * RW + rw, x);
         add_up();
-#pragma unroll
-        for (int b = 0; b < KB; ++b) s[b] = x[b];
+        s = x;
       }
       u_last = u;
     }
@@ -158,24 +144,19 @@ __global__ void __launch_bounds__(64 * KW * RW, 2) weigh_bf16_kernel(WeighParams
     mask(u_last);
     add_up();
   }
-#pragma unroll
-  for (int b = 0; b < KB; ++b) sum[b] = pair_sum(sum[b]);
+  sum = pair_sum(sum);
   if constexpr (RW > 1) {
     float* part = reinterpret_cast<float*>(q_lds);  // (behind the last barrier)
-    if (h == 0) {
-#pragma unroll
-      for (int b = 0; b < KB; ++b) part[(rw * KW + kw) * (32 * KB) + 32 * b + c32] = sum[b];
-    }
+    if (h == 0) part[(rw * KW + kw) * 32 + c32] = sum;
     __syncthreads();
-    if (tid < KW * 32 * KB) {
+    if (tid < KW * 32) {
       float x = part[tid];
 #pragma unroll
-      for (int i = 1; i < RW; ++i) x += part[i * (KW * 32 * KB) + tid];
+      for (int i = 1; i < RW; ++i) x += part[i * (KW * 32) + tid];
       give(p, g, wg_key + tid, x);
     }
   } else if (h == 0) {
-#pragma unroll
-    for (int b = 0; b < KB; ++b) give(p, g, key0 + 32 * b + c32, sum[b]);
+    give(p, g, key, sum);
   }
 }
 
@@ -183,7 +164,7 @@ template <int D, int KW, int RW, int UB>
 static void launch_many(const WeighParams& p, hipStream_t s) {
   constexpr int keys = 32 * KW;
   const dim3 grid((unsigned)((p.len + keys - 1) / keys), (unsigned)p.n_kv_heads), block(64 * KW * RW);
-  hipLaunchKernelGGL((weigh_bf16_kernel<D, 1, KW, RW, UB>), grid, block, 0, s, p);
+  hipLaunchKernelGGL((weigh_bf16_kernel<D, KW, RW, UB>), grid, block, 0, s, p);
 }
 
 // At most 16 rows, bf16: every wavefront takes strips of 64 keys.
