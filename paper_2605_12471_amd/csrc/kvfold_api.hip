@@ -669,7 +669,7 @@ int kvfold_cache_evict(kvfold_cache_t* c, int layer, const float* weights, int64
   for (int i = 0; i < 5; ++i) {
     if (!out[i].bytes) continue;
     for (int j = 0; j < 3; ++j) {
-      const bool own_rows = in_place && i >= 3 && j >= 1, own_weights = i == 2 && j == 0;
+      const bool own_rows = in_place && i >= 3 && j >= 1, own_weights = i == 2 && j == 0 && to_weights == weights;
       ok = ok && (own_rows || own_weights || apart(out[i].at, out[i].bytes, in[j].at, in[j].bytes));
     }
     for (int j = 0; j < i; ++j) ok = ok && (!out[j].bytes || apart(out[i].at, out[i].bytes, out[j].at, out[j].bytes));

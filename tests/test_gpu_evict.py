@@ -375,3 +375,43 @@ def test_refusals():
     assert cache.length(0) == 100
     with pytest.raises(ValueError):
         cache.evict(0, w, 10, kept=torch.empty((2, 9), dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.parametrize("n", [1, 20])
+def test_caches_whose_places_pass_32_bits(n):
+    """Rows that are all alike, and 100 others behind them: 20 GB of rows, 160 MB of weights."""
+    heads, d, same = 40, 128, 1_000_000
+    length = same + 100
+    cache = kv.KvFoldCache(1, heads, heads, d, 64, length + 28)
+    first, tail = [draw((heads, 1, d), seed) for seed in (1, 2)], [draw((heads, 100, d), seed) for seed in (3, 4)]
+    for view, x, y in zip(cache.view(0), first, tail):
+        view[:, :same].copy_(x.cuda().expand(heads, same, d))
+        view[:, same:length].copy_(y)
+    cache.set_length(0, length)
+    q, lse = draw((n, heads, d), 5), torch.full((heads, n), 14.0)
+    weights = torch.full((heads, length + 28), 7.0, device="cuda")
+    cache.weigh(0, q.cuda(), lse.cuda(), weights, add=False)
+    want, tol = reference_weights(q, torch.cat((first[0], tail[0]), 1), lse, d, 1)
+    got = torch.cat((weights[:, :1], weights[:, same:length]), 1).cpu().double().numpy()
+    assert (np.abs(got - want) <= tol).all()
+    assert (weights[:, :same] == weights[:, :1]).all() and (weights[:, length:] == 7).all()
+    order = torch.sort(weights[:, 4:length - 10], dim=1, descending=True, stable=True).indices[:, :66] + 4
+    ends = torch.cat((torch.arange(4), torch.arange(length - 10, length))).cuda().expand(heads, 14)
+    expected = torch.sort(torch.cat((order, ends), 1), dim=1).values
+    rows = [torch.gather(view, 1, expected[:, :, None].expand(heads, 80, d)) for view in cache.view(0)]
+    for to in (kv.KvFoldCache(1, heads, heads, d, 64, 100), None):
+        kept = torch.empty((heads, 80), dtype=torch.int32, device="cuda")
+        cache.evict(0, weights, 80, 4, 10, to=to, kept=kept)
+        assert torch.equal(kept.long(), expected)
+        for view, x in zip((to or cache).view(0), rows):
+            assert torch.equal(view[:, :80], x)
+    assert cache.length(0) == 80
+
+
+def test_kept_weights_lie_on_the_weights_or_apart():
+    cache, _, _ = filled(4, 2, 64, 100)
+    w = torch.rand((2 * 100 + 50,), device="cuda")
+    space = torch.empty((cache.evict_workspace_bytes(60),), dtype=torch.uint8, device="cuda")
+    call = lambda to: kv.kvfold_cache_evict(cache.handle, 0, w.data_ptr(), 60, 0, 0, None, 0, to, None, space.data_ptr(), space.numel())
+    assert call(w.data_ptr() + 4) == -1 and call(w.data_ptr() + 4 * 50) == -1 and cache.length(0) == 100
+    assert call(w.data_ptr()) == 0 and cache.length(0) == 60

@@ -387,3 +387,39 @@ def test_refusals():
         f.cache.append(0, k, v.transpose(0, 1).contiguous().transpose(0, 1))
     f.cache.append(0, k[:0], v[:0])
     assert f.cache.length(0) == 70
+
+
+@pytest.mark.parametrize("hq,hkv,d,same", [(40, 40, 128, 1_000_000), (4, 1, 64, 33_554_240)])
+@pytest.mark.parametrize("n", [1, 20])
+def test_caches_whose_places_pass_32_bits(hq, hkv, d, same, n):
+    """Rows that are all alike, 5 GB of codes or 2 GiB of a head's, and 60 + n others behind them, which get the larger part of the weight."""
+    cache = kv.KvFoldQuantCache(1, hq, hkv, d, 64, same + 128)
+    first = [draw((1, hkv, d), seed) for seed in (1, 2)]
+    cache.append(0, *(x.cuda().expand(same, hkv, d) for x in first))
+    tail = [draw((60 + n, hkv, d), seed) for seed in (3, 4)]
+    cache.append(0, *(x[:60].cuda() for x in tail))
+    q = draw((n, hq, d), 5, 6.0)
+    out, lse = torch.empty((n, hq, d), dtype=torch.bfloat16, device="cuda"), torch.empty((hq, n), device="cuda")
+    cache.step(0, q.cuda(), *(x[60:].cuda() for x in tail), out, lse=lse)
+    assert cache.length(0) == same + 60 + n
+    one = [R.held(x.expand(64, hkv, d).float().numpy())[:1] for x in first]
+    others = [R.held(x.float().numpy()) for x in tail]
+    for begin, ref in ((0, one), (same // 2 + 5, one), (same - 1, [np.concatenate(x) for x in zip(one, others)])):
+        got = [torch.empty(ref[0].shape, device="cuda") for _ in range(2)]
+        cache.read(0, begin, *got)
+        for x, y in zip(got, ref):
+            assert np.array_equal(x.cpu().numpy(), y.astype(np.float32))
+    k, v = (np.concatenate(x) for x in zip(one, others))
+    seen = np.arange(61 + n)[None, :] <= 61 + np.arange(n)[:, None]
+    times = np.where(np.arange(61 + n) == 0, float(same), 1.0)
+    ref, mean_abs, ref_lse, span = np.empty((n, hq, d)), np.empty((n, hq, d)), np.empty((hq, n)), np.empty((hq, n))
+    for h in range(hq):
+        g, qq = h // (hq // hkv), q[:, h].double().numpy()
+        s, a = qq @ k[:, g].T / math.sqrt(d), np.abs(qq) @ np.abs(k[:, g]).T / math.sqrt(d)
+        top = np.where(seen, s, -np.inf).max(-1, keepdims=True)
+        p = np.where(seen, times * np.exp(s - top), 0)
+        total = p.sum(-1, keepdims=True)
+        ref_lse[h], span[h] = (top + np.log(total))[:, 0], np.where(seen, a, 0).max(-1)
+        ref[:, h], mean_abs[:, h] = p / total @ v[:, g], p / total @ np.abs(v[:, g])
+    tol, tol_lse = R.bounds(ref, ref_lse, mean_abs, span, d, same + 60 + n)
+    assert (np.abs(out.cpu().double().numpy() - ref) <= tol).all() and (np.abs(lse.cpu().double().numpy() - ref_lse) <= tol_lse).all()
