@@ -11,6 +11,10 @@
 // its share of O the codes times P', rounded to bf16 for the matrix instruction as in the other kernels, and its share of the row sum P' / v,
 // whose factor is taken out of the block's sum.  So neither the queries nor the keys are rounded on the way.  m is the row's maximum, stale by
 // at most 2^16; O, m and l are fp32.
+//
+// A step whose rows fill no block is one launch: the wavefront that has the incomplete block writes the new rows into it, waits for its own stores and
+// reads them back; nobody else reads them.  (The append as a launch in front takes 4.7 us.)  One token, 32 heads on 8, 128 wide, captured steps: 300
+// keys 6.7 us, 4187 7.5, 16K 10.1, 128K 46 (268 MB of codes, 5.8 TB/s).
 #include "meet.h"
 #include "qcache.h"
 
