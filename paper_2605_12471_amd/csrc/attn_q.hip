@@ -1,5 +1,5 @@
 // Chunk-prefix attention on a cache held in 8 bits, any number of rows.  A work unit is 32 consecutive packed (token, head of the group) rows
-// of a KV head, the work of one wavefront; a workgroup has NW of them of one KV head, eight where heads are 128 wide, and a piece of its blocks.
+// of a KV head, the work of one wavefront; a workgroup has NW of them of one KV head, and a piece of its blocks.
 //
 // Bound by the matrix instructions and by issue.  A block of 64 keys is brought in as codes, half the bytes of bf16; each thread widens its own to
 // bf16, which holds them exactly, and puts them into LDS in the order of the matrix instructions' operands, so that they are widened once for
@@ -14,7 +14,7 @@
 //
 // A turn of a SIMD's two wavefronts, 64 matrix instructions of 32 cycles, takes 1.9 us, 0.58 of what the pipes do alone; the rest is issue: per logit a
 // multiplication, an exponential, an addition and half a rounding, and the widening.  Steps of 32 heads on 8, 128 wide: 256 tokens on 64K keys 270 us
-// (1.02 PFLOP/s), 2048 on 32K 1030 us (1.10); 64 wide, 1000 on 8K, where a logit has half the products, 112 us (0.63).  Codes three turns ahead
+// (1.02 PFLOP/s), 2048 on 32K 1030 us (1.10); 64 wide, 1000 on 8K, where a logit has half the products, 102 us (0.69).  Codes three turns ahead
 // by copies to LDS took as long (1033 us), and so did codes of one place for every block: it is not the memory that is waited for.
 #include "qcache.h"
 #include "wave_ops.h"
@@ -32,11 +32,11 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
   const AttnParams& p = qp.a;
   constexpr int KS = D / 16, JT = D / 32;            // contraction steps of S^T, tiles of O^T
   constexpr int BLOCK = kQBlock * D;                 // codes of a block
-  constexpr int NT = NW * 64, T = BLOCK / 16 / NT;   // threads; pieces of K, and of V, of each
+  constexpr int NT = NW * 64, T = 2 * BLOCK / 16 / NT;  // threads; pieces of each: one of K and one of V, or of either
   constexpr int SLOT = BLOCK * 2;                    // bytes of a block's K, or V, in LDS
   constexpr float kStale = 16.0f;                    // log2 units
   constexpr float kFar = 0x1p60f, kLost = 0x1p100f;  // sums of a lane's weights in a block
-  static_assert(T * NT * 16 == BLOCK, "every thread has the same share of a block");
+  static_assert(T * NT * 16 == 2 * BLOCK && (T == 1 || T == 2), "every thread has the same share of a block");
   __shared__ __attribute__((aligned(16))) unsigned char lds[4 * SLOT];  // K, K, V, V
 
   const int lid = logical_workgroup(blockIdx.x, gridDim.x, p);
@@ -78,57 +78,46 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
   // ---- a block on its way: K fragment (tile t, step, half) at ((t KS + step) 2 + half) 512, V fragment (tile t, step, tile of O^T, half) at
   // (((t 2 + step) JT + tile) 2 + half) 512, in two slots of each.  (By buffer accesses: a lane's place in a block is fixed and the
   // block's is a scalar.  A head's codes take at most 2^31 bytes.)
-  __amdgpu_buffer_rsrc_t codes[2];
+  // Piece j of a thread is K's (v = 0) or V's (v = 1), number `mine` of the block.
+  auto v_of = [&](int j) __attribute__((always_inline)) -> int { return T == 2 ? j : w / (NW / 2); };
+  const unsigned mine = T == 2 ? (unsigned)tid : (unsigned)tid % (NT / 2);
+  __amdgpu_buffer_rsrc_t codes[T];
 #pragma unroll
-  for (int v = 0; v < 2; ++v)
-    codes[v] = __builtin_amdgcn_make_buffer_rsrc(qp.c.codes[v] + (uint64_t)g * (uint64_t)qp.c.blocks * BLOCK, 0, (unsigned)qp.c.blocks * (unsigned)BLOCK, 0x00020000);
+  for (int j = 0; j < T; ++j)
+    codes[j] = __builtin_amdgcn_make_buffer_rsrc(qp.c.codes[v_of(j)] + (uint64_t)g * (uint64_t)qp.c.blocks * BLOCK, 0, (unsigned)qp.c.blocks * (unsigned)BLOCK, 0x00020000);
   const float* scales = qp.c.scales + 2 * (uint64_t)g * (uint64_t)qp.c.blocks;
-  quintx4 raw[2][T];
-  auto load = [&](int v, int b) __attribute__((always_inline)) {
-#pragma unroll
-    for (int j = 0; j < T; ++j)
-      raw[v][j] = __builtin_bit_cast(quintx4, __builtin_amdgcn_raw_buffer_load_b128(codes[v], (unsigned)tid * 16, (unsigned)b * (unsigned)BLOCK + (unsigned)(NT * j) * 16, 0));
+  quintx4 raw[T];
+  auto load = [&](int j, int b) __attribute__((always_inline)) {
+    raw[j] = __builtin_bit_cast(quintx4, __builtin_amdgcn_raw_buffer_load_b128(codes[j], mine * 16, (unsigned)b * (unsigned)BLOCK, 0));
   };
-  auto put_half = [&](int v, int b, int piece, int half, const qbf16x8& x) __attribute__((always_inline)) {
-    unsigned char* at = lds + (2 * v + (b & 1)) * SLOT;
-    if (v == 0) {
-      const int c = piece >> 6, key = piece & 63;
-      at += ((((key >> 5) * KS + c) * 2 + half) * 32 + (key & 31)) * 16;
-    } else {
-      const int kg = piece / D, col = piece % D;
-      at += (((((kg >> 1) * 2 + half) * JT + (col >> 5)) * 2 + (kg & 1)) * 32 + (col & 31)) * 16;
-    }
-    *reinterpret_cast<qbf16x8*>(at) = x;
+  auto put_half = [&](int j, int b, unsigned piece, int half, const qbf16x8& x) __attribute__((always_inline)) {
+    const int v = v_of(j);
+    const unsigned c = piece >> 6, key = piece & 63, kg = piece / D, col = piece % D;
+    const unsigned in_k = (((key >> 5) * KS + c) * 2 * 32 + (key & 31)) * 16, in_v = ((((kg >> 1) * 2 * JT + (col >> 5)) * 2 + (kg & 1)) * 32 + (col & 31)) * 16;
+    *reinterpret_cast<qbf16x8*>(lds + ((v ? in_v : in_k) + (unsigned)((2 * v + (b & 1)) * SLOT + half * (v ? JT * 1024 : 512)))) = x;
   };
   // Asks for block b, and puts what was asked for into LDS, as far as there is such a block
-  auto load_any = [&](int v, int b) __attribute__((always_inline)) {
-    if (b < b_codes) load(v, b);
+  auto load_any = [&](int j, int b) __attribute__((always_inline)) {
+    if (b < b_codes) load(j, b);
   };
-  auto store_any = [&](int v, int b) __attribute__((always_inline)) {
-    int me = tid;
+  auto store_any = [&](int j, int b) __attribute__((always_inline)) {
+    unsigned me = mine;
     asm volatile("" : "+v"(me));  // (or what follows from it would be held in registers all the while)
     if (b < b_codes) {
 #pragma unroll
-      for (int j = 0; j < T; ++j)
-#pragma unroll
-        for (int half = 0; half < 2; ++half) put_half(v, b, me + NT * j, half, q_widen_half(raw[v][j], half));
+      for (int half = 0; half < 2; ++half) put_half(j, b, me, half, q_widen_half(raw[j], half));
     } else if (b < b_end) {
       // the rows that are not a whole block, in bf16; places without a row hold anything, in V they become 0 (0 times it has to be 0)
-      const int n = len - b * kQBlock;
-      const uint64_t slot = ((uint64_t)g * kQRing + (unsigned)b % kQRing) * BLOCK;
-#pragma unroll 1
-      for (int j = 0; j < T; ++j) {
-        const int piece = me + NT * j, kg = piece / D;
-        const qbf16x8* at = reinterpret_cast<const qbf16x8*>(qp.c.ring[v] + slot + piece * 16);
-        qbf16x8 x[2] = {at[0], at[1]};
-        if (v == 1) {
+      const int n = len - b * kQBlock, kg = (int)(me / D);
+      const qbf16x8* at = reinterpret_cast<const qbf16x8*>(qp.c.ring[v_of(j)] + ((uint64_t)g * kQRing + (unsigned)b % kQRing) * BLOCK + me * 16);
+      qbf16x8 x[2] = {at[0], at[1]};
+      if (v_of(j) == 1) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (32 * (kg >> 1) + 4 * (kg & 1) + 8 * (e >> 2) + (e & 3) >= n) x[e >> 3][e & 7] = (__bf16)0.f;
-        }
-        put_half(v, b, piece, 0, x[0]);
-        put_half(v, b, piece, 1, x[1]);
+        for (int e = 0; e < 16; ++e)
+          if (32 * (kg >> 1) + 4 * (kg & 1) + 8 * (e >> 2) + (e & 3) >= n) x[e >> 3][e & 7] = (__bf16)0.f;
       }
+#pragma unroll
+      for (int half = 0; half < 2; ++half) put_half(j, b, me, half, x[half]);
     }
   };
 
@@ -217,7 +206,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
   bool lost = false;
   auto turn = [&](const floatx16 (&s)[2], floatx16 (&x)[2], int b, float to_log2, float v_scale) __attribute__((always_inline)) {
     constexpr int SM = 2 * KS, OM = 4 * JT, NS = SM + OM, kAhead = 2;
-    constexpr int WORDS = 2 * T * 8, E = NS - NS / 8;  // words of widened codes; slots with exponentials
+    constexpr int WORDS = T * 8, E = NS - NS / 8;  // words of widened codes; slots with exponentials
     const unsigned char *kbuf = lds + ((b + 1) & 1) * SLOT + l * 16, *vbuf = lds + (2 + (b & 1)) * SLOT + l * 16;
     auto operand = [&](int i) __attribute__((always_inline)) -> qbf16x8 {  // of slot i
       return *reinterpret_cast<const qbf16x8*>(i < SM ? kbuf + ((i & 1) * KS + (i >> 1)) * 1024 : vbuf + (i - SM) * 1024);
@@ -253,14 +242,13 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
       }
 #pragma unroll
       for (int k = WORDS * i / NS; k < WORDS * (i + 1) / NS; ++k) {
-        const int v = k / (8 * T), piece = k / 8 % T;
-        wide[k % 4] = q_widen_word(raw[v][piece], k % 8);
-        if (k % 4 == 3) put_half(v, b + 2 - v, tid + NT * piece, k / 4 % 2, __builtin_bit_cast(qbf16x8, wide));
+        wide[k % 4] = q_widen_word(raw[k / 8], k % 8);
+        if (k % 4 == 3) put_half(k / 8, b + 2 - v_of(k / 8), mine, k / 4 % 2, __builtin_bit_cast(qbf16x8, wide));
       }
-      if (i == NS / 2) load(0, b + 3);
+      if (T == 2 && i == NS / 2) load(0, b + 3);
       __builtin_amdgcn_sched_barrier(0);
     }
-    load(1, b + 2);
+    load(T - 1, b + 3 - v_of(T - 1));
     l_run = __builtin_fmaf(sum, inv_v, l_run);
     if (__builtin_expect(__any(!(sum * inv_v < kFar)), 0)) {
       // Logits far above their row's reference: it follows by a power of two.  Beyond what fp32 holds all is to be done again.
@@ -296,14 +284,17 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
   };
 #pragma unroll 1
   for (bool again = false; b_begin < b_end; again = true) {  // the second time, if there is one, with every block's maximum
-    load_any(0, b_begin);
-    load_any(1, b_begin);
-    store_any(0, b_begin);
-    store_any(1, b_begin);
-    load_any(0, b_begin + 1);
-    store_any(0, b_begin + 1);
-    load_any(0, b_begin + 2);
-    load_any(1, b_begin + 1);
+#pragma unroll
+    for (int j = 0; j < T; ++j) load_any(j, b_begin);
+#pragma unroll
+    for (int j = 0; j < T; ++j) {
+      store_any(j, b_begin);
+      if (v_of(j) == 0) {
+        load_any(j, b_begin + 1);
+        store_any(j, b_begin + 1);
+      }
+      load_any(j, b_begin + 2 - v_of(j));
+    }
     scale = scale_of(b_begin);
     __syncthreads();
     logits(s, b_begin);
@@ -320,10 +311,11 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
     }
 #pragma unroll 1
     for (; b < b_end; ++b) {
-      store_any(0, b + 2);
-      store_any(1, b + 1);
-      load_any(0, b + 3);
-      load_any(1, b + 2);
+#pragma unroll
+      for (int j = 0; j < T; ++j) {
+        store_any(j, b + 2 - v_of(j));
+        load_any(j, b + 3 - v_of(j));
+      }
       if (b * kQBlock < vis_last) {
         const float to_log2 = q_to_log2(scale.x, p.scale_log2e);
         reference(s, b, to_log2);
@@ -377,12 +369,14 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
   }
 }
 
-hipError_t launch_attn_q(const QAttnParams& p, int head_dim, hipStream_t s) {
-  const dim3 grid(padded_grid(p.a.n_wgs));
+hipError_t launch_attn_q(const QAttnParams& p, int head_dim, int waves, hipStream_t s) {
+  const dim3 grid(padded_grid(p.a.n_wgs)), block(waves * 64);
   if (head_dim == 128)
-    hipLaunchKernelGGL((attn_q_kernel<128, 8>), grid, dim3(512), 0, s, p);
+    hipLaunchKernelGGL((attn_q_kernel<128, 8>), grid, block, 0, s, p);
+  else if (waves == 8)
+    hipLaunchKernelGGL((attn_q_kernel<64, 8>), grid, block, 0, s, p);
   else
-    hipLaunchKernelGGL((attn_q_kernel<64, 4>), grid, dim3(256), 0, s, p);
+    hipLaunchKernelGGL((attn_q_kernel<64, 4>), grid, block, 0, s, p);
   return hipGetLastError();
 }
 

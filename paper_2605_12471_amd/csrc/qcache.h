@@ -116,7 +116,7 @@ struct QAttnParams {
   const __bf16 *k_new, *v_new;
 };
 hipError_t launch_attn_qdecode(const QAttnParams& p, int head_dim, hipStream_t s);
-hipError_t launch_attn_q(const QAttnParams& p, int head_dim, hipStream_t s);
+hipError_t launch_attn_q(const QAttnParams& p, int head_dim, int waves, hipStream_t s);  // waves: of a workgroup, as planned
 
 typedef __attribute__((ext_vector_type(8))) __bf16 qbf16x8;
 typedef __attribute__((ext_vector_type(4))) unsigned quintx4;

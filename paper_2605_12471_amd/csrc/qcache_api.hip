@@ -240,7 +240,7 @@ int kvfold_qcache_step(kvfold_qcache_t* c, int layer, const void* q, const void*
   const int64_t row = (int64_t)f.n_kv_heads * f.head_dim;
   hipError_t e = inside ? hipSuccess : append(c, layer, k_new, v_new, row, f.head_dim, n_tokens, rope_cos, rope_sin, s);
   if (e != hipSuccess) return hip_fail(e);
-  e = pl.decode ? launch_attn_qdecode(p, f.head_dim, s) : launch_attn_q(p, f.head_dim, s);
+  e = pl.decode ? launch_attn_qdecode(p, f.head_dim, s) : launch_attn_q(p, f.head_dim, pl.waves_per_wg, s);
   if (e != hipSuccess) return hip_fail(e);
   if (pl.n_splits > 1 && !meet) {
     CombineParams cp;

@@ -29,10 +29,15 @@ QPlan make_qplan(const kvfold_config_t& c, int n_cu, int64_t ws_rows, int n_toke
   QPlan pl{};
   pl.decode = rows <= 16;
   pl.units_per_head = units_of_head(n_tokens, G);
-  pl.waves_per_wg = c.head_dim == 128 ? 8 : 4;
+  // Chunks: eight wavefronts share what is widened, four come sooner to their end and leave fewer pieces to merge.  64 wide, eight where workgroups of
+  // four on every CU would have more than 32 blocks each: 32 heads on 8, 1000 tokens on 8K keys (141 blocks) 103 us, in fours 111 to 122, 100 on 16K (32.3) 35.3, 38.4; 512 on
+  // 2048 (20) 36.1, in fours 33.7, on 512 (8) 28.3, 24.3; 4 heads on 1, 256 on 4096 (8.5) 22.0, 18.9.  Up to four units the other four wavefronts only widen:
+  // 20 tokens on 32K 27.0, in fours 28.3.  128 wide a workgroup of four has no registers for its share.
+  const int64_t blocks_of_fours = (int64_t)c.n_kv_heads * ((pl.units_per_head + 3) / 4) * blocks;
+  pl.waves_per_wg = c.head_dim == 64 && pl.units_per_head > 4 && blocks_of_fours <= (int64_t)32 * n_cu ? 4 : 8;
   pl.wgs_per_head = pl.decode ? 1 : (pl.units_per_head + pl.waves_per_wg - 1) / pl.waves_per_wg;
   const int64_t per_split = (int64_t)c.n_kv_heads * pl.wgs_per_head;
-  int64_t splits = pl.decode ? decode_splits(blocks, std::min<int64_t>(std::max<int64_t>(1, n_cu / c.n_kv_heads), kMaxSplits)) : std::min<int64_t>((c.head_dim == 128 ? 1 : 2) * (int64_t)n_cu / per_split, blocks);
+  int64_t splits = pl.decode ? decode_splits(blocks, std::min<int64_t>(std::max<int64_t>(1, n_cu / c.n_kv_heads), kMaxSplits)) : std::min<int64_t>((int64_t)n_cu / per_split, blocks);
   splits = std::min<int64_t>(splits, kMaxSplits);
   splits = std::min(splits, ws_rows / ((int64_t)n_tokens * c.n_q_heads));
   splits = std::max<int64_t>(splits, 1);

@@ -423,3 +423,11 @@ def test_caches_whose_places_pass_32_bits(hq, hkv, d, same, n):
         ref[:, h], mean_abs[:, h] = p / total @ v[:, g], p / total @ np.abs(v[:, g])
     tol, tol_lse = R.bounds(ref, ref_lse, mean_abs, span, d, same + 60 + n)
     assert (np.abs(out.cpu().double().numpy() - ref) <= tol).all() and (np.abs(lse.cpu().double().numpy() - ref_lse) <= tol_lse).all()
+
+
+@pytest.mark.parametrize("prev,n", [(24_010, 65), (24_640, 130)])
+def test_eight_wavefronts_64_wide(prev, n):
+    f = Fold(40, 2, 64, prev + n, seed=9)
+    f.append(prev)
+    f.step(n)
+    f.check_rows(first=prev - 70)
