@@ -98,16 +98,16 @@ __device__ __forceinline__ void append_block(const QAppendParams& p, int g) {
   Piece<D, V> q[T];
 #pragma unroll
   for (int j = 0; j < T; ++j) q[j] = piece_in<D, V>(p, block, g, tid + j * kThreads);
-  // The ring takes the rows of the last two blocks.  Whose slot the first block's earlier rows lie in is written by the first block's
+  // The ring takes the rows of the last two blocks.  Whose slot the first block's earlier rows lie in, if it has any, is written by the first block's
   // workgroup, once it has read them.
-  const bool later = block != first && (block - first) % kQRing == 0;
+  const bool earlier = p.len_prev % kQBlock != 0, later = earlier && block != first && (block - first) % kQRing == 0;
   if (block + kQRing > last && !later) {
 #pragma unroll
     for (int j = 0; j < T; ++j) to_ring<D, V>(ring + (block % kQRing) * (kQBlock * D), tid + j * kThreads, q[j]);
   }
   const bool whole = (block + 1) * kQBlock <= end;
   if (whole) {
-    if (block == first && p.len_prev % kQBlock) {
+    if (block == first && earlier) {
       const unsigned short* slot = reinterpret_cast<const unsigned short*>(ring) + (block % kQRing) * (kQBlock * D);
 #pragma unroll
       for (int j = 0; j < T; ++j) {
@@ -152,7 +152,7 @@ __device__ __forceinline__ void append_block(const QAppendParams& p, int g) {
   }
   // The block whose rows take the place of the first block's in the ring
   const int64_t over = last - (last - first) % kQRing;
-  if (block == first && over > first) {
+  if (block == first && earlier && over > first) {
     __syncthreads();  // (the block's earlier rows have been read: their values went into the codes' scale)
 #pragma unroll 1
     for (int j = 0; j < T; ++j) to_ring<D, V>(ring + (over % kQRing) * (kQBlock * D), tid + j * kThreads, piece_in<D, V>(p, over, g, tid + j * kThreads));

@@ -431,3 +431,19 @@ def test_eight_wavefronts_64_wide(prev, n):
     f.append(prev)
     f.step(n)
     f.check_rows(first=prev - 70)
+
+
+@pytest.mark.parametrize("prev", [0, 64, 128, 100])
+@pytest.mark.parametrize("n", [64, 65, 128, 130, 192, 193, 256, 300])
+def test_rows_taken_back_behind_a_chunk(prev, n):
+    """The last blocks' rows are in bf16 wherever the chunk began."""
+    f = Fold(8, 2, 128, prev + n + 64, seed=prev + n)
+    f.append(prev)
+    f.append(n)
+    for back in (1, 37, 64):
+        f.cache.truncate(0, prev + n - back)
+        f.k, f.v = f.k[:prev + n - back], f.v[:prev + n - back]
+        f.check_rows()
+        f.append(back)
+    f.step(2)
+    f.check_rows()
