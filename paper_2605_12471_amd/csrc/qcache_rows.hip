@@ -1,9 +1,9 @@
 // Rows on their way into the cache that is held in 8 bits, and back (the layout and the arithmetic are described in qcache.h).
 //
 // Append: a workgroup has a block of 64 rows of one KV head, K or V.  Rows that were there already come from the ring, the others as handed
-// in; the block's largest magnitude is found, and the codes leave 16 bytes a lane.  Memory-bound where many rows come at once (8 heads, 128 wide: 131072 rows 226 us,
-// 3.6 TB/s), else one launch's latency (up to 64 rows 4.7 us, 256 8.5, 2048 11).  Reading
-// back is memory-bound as well, four bytes written for a code: 65536 rows 133 us, 5.0 TB/s.
+// in; the block's largest magnitude is found, and the codes leave 16 bytes a lane.  Memory-bound where many rows come at once (8 heads, 128 wide: 65536 rows 108 us,
+// 3.7 TB/s), else one launch's latency (up to 64 rows 4.7 us, 256 6.0, 2048 8.3).  Reading
+// back is memory-bound as well, four bytes written for a code: 65536 rows 133 to 137 us, 5.0 TB/s.
 #include "qcache.h"
 
 namespace kvfold {
