@@ -51,29 +51,37 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
   const int C = p.n_tokens, Hq = p.n_q_heads, G = p.group, rows = C * G;
   const int len = (int)p.len_prev + C, n_whole = len / kQBlock;
 
+  // Keys that a row sees; that the workgroup's last row sees
+  auto seen_by = [&](int r) __attribute__((always_inline)) -> int {
+    r = r < rows ? r : rows - 1;
+    return (int)p.len_prev + (int)quot((unsigned)r, p.by_group) + 1;
+  };
+  const int vis_wg = seen_by((wg + 1) * NW * kRowsPerUnit - 1);
+  const int b_begin = split * p.tiles_per_split, b_seen = (vis_wg + kQBlock - 1) / kQBlock;
+  const int b_end = b_begin + p.tiles_per_split < b_seen ? b_begin + p.tiles_per_split : b_seen;
+  const int b_codes = b_end < n_whole ? b_end : n_whole;  // blocks before it are held as codes
+
+  // ---- the chunk's rows, where they are appended here: the head's only workgroup with its last block writes them, and reads them back behind a barrier
+  if (qp.k_new && b_begin <= n_whole && n_whole < b_end) {
+    q_fill_block<D>(qp, g, ((uint64_t)g * kQRing + (unsigned)n_whole % kQRing) * BLOCK, len - n_whole * kQBlock, tid, NT);
+    __syncthreads();
+  }
+
   // ---- the wavefront's rows: lane (c32, h) holds columns 16 ks + 8 h .. + 7 of row c32
   const int unit = wg * NW + w;
-  int my_vis;
+  int my_vis;  // keys that the lane's row sees, counted from the lane's first of a block
   qbf16x8 qf[KS];
   {
     const int r = unit * kRowsPerUnit + c32, row = r < rows ? r : rows - 1, tok = (int)quot((unsigned)row, p.by_group);
-    my_vis = (int)p.len_prev + tok + 1;
+    my_vis = (int)p.len_prev + tok + 1 - 4 * h;
     const __bf16* qrow = reinterpret_cast<const __bf16*>(p.q) + (uint64_t)(unsigned)(row + tok * (Hq - G) + g * G) * D;
     const float* cs = p.rope_cos ? p.rope_cos + (int64_t)tok * (D / 2) : nullptr;
     const float* sn = p.rope_cos ? p.rope_sin + (int64_t)tok * (D / 2) : nullptr;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[ks] = q_query<D>(qrow, 16 * ks + 8 * h, cs, sn);
   }
-  // Keys that the wavefront's first row sees, and its last one; that the workgroup's last row sees
-  auto seen_by = [&](int r) __attribute__((always_inline)) -> int {
-    r = r < rows ? r : rows - 1;
-    return (int)p.len_prev + (int)quot((unsigned)r, p.by_group) + 1;
-  };
+  // Keys that the wavefront's first row sees, and its last one
   const int vis_first = seen_by(unit * kRowsPerUnit), vis_last = unit * kRowsPerUnit < rows ? seen_by((unit + 1) * kRowsPerUnit - 1) : 0;
-  const int vis_wg = seen_by((wg + 1) * NW * kRowsPerUnit - 1);
-  const int b_begin = split * p.tiles_per_split, b_seen = (vis_wg + kQBlock - 1) / kQBlock;
-  const int b_end = b_begin + p.tiles_per_split < b_seen ? b_begin + p.tiles_per_split : b_seen;
-  const int b_codes = b_end < n_whole ? b_end : n_whole;  // blocks before it are held as codes
 
   // ---- a block on its way: K fragment (tile t, step, half) at ((t KS + step) 2 + half) 512, V fragment (tile t, step, tile of O^T, half) at
   // (((t 2 + step) JT + tile) 2 + half) 512, in two slots of each.  (By buffer accesses: a lane's place in a block is fixed and the
@@ -85,7 +93,9 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
 #pragma unroll
   for (int j = 0; j < T; ++j)
     codes[j] = __builtin_amdgcn_make_buffer_rsrc(qp.c.codes[v_of(j)] + (uint64_t)g * (uint64_t)qp.c.blocks * BLOCK, 0, (unsigned)qp.c.blocks * (unsigned)BLOCK, 0x00020000);
-  const float* scales = qp.c.scales + 2 * (uint64_t)g * (uint64_t)qp.c.blocks;
+  // (scales by scalar loads: nobody writes them meanwhile)
+  typedef const __attribute__((address_space(4))) floatx2* constants;
+  const constants scales = (constants)(uintptr_t)(qp.c.scales + 2 * (uint64_t)g * (uint64_t)qp.c.blocks);
   quintx4 raw[T];
   auto load = [&](int j, int b) __attribute__((always_inline)) {
     raw[j] = __builtin_bit_cast(quintx4, __builtin_amdgcn_raw_buffer_load_b128(codes[j], mine * 16, (unsigned)b * (unsigned)BLOCK, 0));
@@ -150,7 +160,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
   auto reference = [&](floatx16 (&s)[2], int b, float to_log2) __attribute__((always_inline)) {
     const int key0 = b * kQBlock;
     if (key0 + kQBlock > vis_first) {  // wave-uniform: some row does not see the whole block
-      const int rel = my_vis - key0 - 4 * h;
+      const int rel = my_vis - key0;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -271,7 +281,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
   floatx16 s[2], x[2];
   floatx2 scale;
   auto step = [&](floatx16 (&now)[2], floatx16 (&next)[2], int b) __attribute__((always_inline)) {
-    const floatx2 scale_next = *reinterpret_cast<const floatx2*>(scales + 2 * (unsigned)(b + 1));
+    const floatx2 scale_next = scales[(unsigned)(b + 1)];
     const float to_log2 = q_to_log2(scale.x, p.scale_log2e);
     // every row sees all of the block, and has a reference
     if (!__all(b * kQBlock + kQBlock <= vis_first && m_run != -INFINITY)) reference(now, b, to_log2);
@@ -280,29 +290,30 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
     __syncthreads();
   };
   auto scale_of = [&](int b) __attribute__((always_inline)) -> floatx2 {
-    return b < b_codes ? *reinterpret_cast<const floatx2*>(scales + 2 * (unsigned)b) : floatx2{1.f, 1.f};
+    return b < b_codes ? scales[(unsigned)b] : floatx2{1.f, 1.f};
   };
 #pragma unroll 1
   for (bool again = false; b_begin < b_end; again = true) {  // the second time, if there is one, with every block's maximum
+    int b = b_begin;
+    asm volatile("" : "+s"(b));  // (or what follows from it would be held in registers for a second time)
 #pragma unroll
-    for (int j = 0; j < T; ++j) load_any(j, b_begin);
+    for (int j = 0; j < T; ++j) load_any(j, b);
 #pragma unroll
     for (int j = 0; j < T; ++j) {
-      store_any(j, b_begin);
+      store_any(j, b);
       if (v_of(j) == 0) {
-        load_any(j, b_begin + 1);
-        store_any(j, b_begin + 1);
+        load_any(j, b + 1);
+        store_any(j, b + 1);
       }
-      load_any(j, b_begin + 2 - v_of(j));
+      load_any(j, b + 2 - v_of(j));
     }
-    scale = scale_of(b_begin);
+    scale = scale_of(b);
     __syncthreads();
-    logits(s, b_begin);
-    __syncthreads();  // (K of block b_begin + 2 is going to take its place)
-    int b = b_begin;
+    logits(s, b);
+    __syncthreads();  // (K of block b + 2 is going to take its place)
     // Turns laid out by hand: a wavefront's that has rows, as long as K of block b + 2 is codes or nobody's.  (Past the piece's end they ask for, and
     // widen, what is never used: codes of other pieces, or zeros, behind the buffer's end; and a scale, of which there is a place behind the last.)
-    // Wavefronts without rows only widen: 37 tokens on 32K keys, five of eight with rows, 51.5 us a step, 56 when they all multiplied.
+    // Wavefronts without rows only widen: 37 tokens on 32K keys, five of eight with rows, 47.5 us a step; 4.5 more when they all multiplied.
     const int b_fast = again || !vis_last ? b : b_codes == b_end ? b_end : b_codes - 2;
 #pragma unroll 1
     for (; b + 1 < b_fast; b += 2) {

@@ -181,20 +181,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attn_qdecode_kernel(QAttnParam
   if (b_rest == n_whole && n_whole < b_end) {
     const int b = n_whole, n = len - b * kQBlock;
     const uint64_t slot = ((uint64_t)g * kQRing + (unsigned)b % kQRing) * BLOCK;
-    if (qp.k_new) {
-      const int64_t stride = (int64_t)p.n_kv_heads * D;
-      const __bf16 *k_new = qp.k_new + g * D, *v_new = qp.v_new + g * D;
-      unsigned short* v_slot = reinterpret_cast<unsigned short*>(qp.c.ring[1] + slot);
-      for (int i = l; i < C * (D / 8); i += 64) {
-        const int t = i / (D / 8), c = i % (D / 8), key = n - C + t;
-        const qbf16x8 k = finite_row(q_query<D>(k_new + t * stride, 8 * c, p.rope_cos ? p.rope_cos + t * (D / 2) : nullptr, p.rope_cos ? p.rope_sin + t * (D / 2) : nullptr));
-        const qbf16x8 v = finite_row(*reinterpret_cast<const qbf16x8*>(v_new + t * stride + 8 * c));
-        *reinterpret_cast<qbf16x8*>(qp.c.ring[0] + slot + q_k_piece(c >> 1, key) * 16 + (c & 1) * 8) = k;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v_slot[q_v_piece(D, q_key_group(key), 8 * c + e) * 16 + q_key_element(key)] = __builtin_bit_cast(unsigned short, (__bf16)v[e]);
-      }
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    }
+    if (qp.k_new) q_fill_block<D>(qp, g, slot, n, l, 64);
     const unsigned char* kb = reinterpret_cast<const unsigned char*>(qp.c.ring[0] + slot) + 2 * k_lane;
     const unsigned char* vb = reinterpret_cast<const unsigned char*>(qp.c.ring[1] + slot) + 2 * v_lane;
     floatx4 s[4];

@@ -112,7 +112,8 @@ hipError_t launch_qread(const QReadParams& p, int head_dim, hipStream_t s);
 struct QAttnParams {
   AttnParams a;  // k_cache, v_cache: unused; tiles_per_split: blocks
   QRows c;
-  // The decoding kernel appends the chunk's rows itself, which fill no block (nullptr: the cache holds them already): as handed in, [C][Hkv][d]
+  // Rows of the chunk that fill no block are appended by whom alone reads them, the workgroup with the head's last block (nullptr: the cache holds them
+  // already): as handed in, [C][Hkv][d]
   const __bf16 *k_new, *v_new;
 };
 hipError_t launch_attn_qdecode(const QAttnParams& p, int head_dim, hipStream_t s);
@@ -170,6 +171,25 @@ __device__ __forceinline__ qbf16x8 q_query(const __bf16* row, int c0, const floa
     rotate_vec<__bf16, 8>(x, other, c, s, c0 < D / 2);
   }
   return x;
+}
+
+// The chunk's rows of KV head g into its incomplete block, in place `slot` of the ring, whose last rows they are of n: share i0, i0 + step, ...
+template <int D>
+__device__ __forceinline__ void q_fill_block(const QAttnParams& qp, int g, uint64_t slot, int n, int i0, int step) {
+  const AttnParams& p = qp.a;
+  const int C = p.n_tokens;
+  const int64_t stride = (int64_t)p.n_kv_heads * D;
+  const __bf16 *k_new = qp.k_new + g * D, *v_new = qp.v_new + g * D;
+  unsigned short* v_slot = reinterpret_cast<unsigned short*>(qp.c.ring[1] + slot);
+  for (int i = i0; i < C * (D / 8); i += step) {
+    const int t = i / (D / 8), c = i % (D / 8), key = n - C + t;
+    const qbf16x8 k = finite_row(q_query<D>(k_new + t * stride, 8 * c, p.rope_cos ? p.rope_cos + t * (D / 2) : nullptr, p.rope_cos ? p.rope_sin + t * (D / 2) : nullptr));
+    const qbf16x8 v = finite_row(*reinterpret_cast<const qbf16x8*>(v_new + t * stride + 8 * c));
+    *reinterpret_cast<qbf16x8*>(qp.c.ring[0] + slot + q_k_piece(c >> 1, key) * 16 + (c & 1) * 8) = k;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v_slot[q_v_piece(D, q_key_group(key), 8 * c + e) * 16 + q_key_element(key)] = __builtin_bit_cast(unsigned short, (__bf16)v[e]);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
 }  // namespace kvfold

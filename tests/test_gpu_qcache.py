@@ -447,3 +447,39 @@ def test_rows_taken_back_behind_a_chunk(prev, n):
         f.append(back)
     f.step(2)
     f.check_rows()
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (32, 8, 64), (28, 4, 128), (40, 2, 64)])
+@pytest.mark.parametrize("prev,n", [(0, 17), (64, 63), (1000, 20), (4187, 32), (4160, 37)])
+@pytest.mark.parametrize("rope", [False, True])
+def test_chunks_that_fill_no_block(hq, hkv, d, prev, n, rope):
+    f = Fold(hq, hkv, d, prev + n + 70, seed=prev + n)
+    f.append(prev)
+    f.step(n, rope=rope)
+    f.check_rows(first=max(0, prev - 70))
+    f.append(70)                       # the block is filled from what the step has left
+    f.check_rows(first=max(0, prev - 70))
+
+
+def test_a_chunk_that_fills_no_block_captured():
+    """Rows, queries and results of another replay, the cache's ring written by each."""
+    f = Fold(8, 2, 128, 600, seed=4)
+    f.append(500)
+    data = [f.chunk(10) for _ in range(3)]
+    q, k, v = (x.cuda() for x in data[0])
+    out = torch.empty_like(q)
+    f.cache.step(0, q, k, v, out)
+    f.cache.truncate(0, 500)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        f.cache.step(0, q, k, v, out)
+    for x, y, z in data + data:
+        q.copy_(x), k.copy_(y), v.copy_(z)
+        graph.replay()
+        got = out.clone()
+        f.cache.truncate(0, 500)
+        again = torch.empty_like(out)
+        f.cache.step(0, q, k, v, again)
+        torch.cuda.synchronize()
+        assert torch.equal(got, again)
