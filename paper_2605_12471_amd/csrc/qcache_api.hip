@@ -1,5 +1,5 @@
-// Host side of the cache held in 8 bits (kvfold_qcache_*): one step = append kernel, attention kernel, and a merge where the keys were cut
-// into pieces that do not meet in the attention kernel.  Stream-ordered; nothing synchronises or allocates after kvfold_qcache_create.
+// Host side of the cache held in 8 bits (kvfold_qcache_*): one step = an append kernel where the attention kernel does not append by itself, the
+// attention kernel, and a merge where the keys were cut into pieces that do not meet in it.  Stream-ordered; nothing synchronises or allocates after kvfold_qcache_create.
 #include <cmath>
 #include <new>
 #include <vector>
