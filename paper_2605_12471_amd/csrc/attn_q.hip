@@ -312,7 +312,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
     logits(s, b);
     __syncthreads();  // (K of block b + 2 is going to take its place)
     // Turns laid out by hand: a wavefront's that has rows, as long as K of block b + 2 is codes or nobody's.  (Past the piece's end they ask for, and
-    // widen, what is never used: codes of other pieces, or zeros, behind the buffer's end; and a scale, of which there is a place behind the last.)
+    // widen, what is never used: what lies behind the piece, at most three blocks further on, which is the layer's own storage: its ring lies behind the codes and scales.)
     // Wavefronts without rows only widen: 37 tokens on 32K keys, five of eight with rows, 47.5 us a step; 4.5 more when they all multiplied.
     const int b_fast = again || !vis_last ? b : b_codes == b_end ? b_end : b_codes - 2;
 #pragma unroll 1
