@@ -483,3 +483,25 @@ def test_a_chunk_that_fills_no_block_captured():
         f.cache.step(0, q, k, v, again)
         torch.cuda.synchronize()
         assert torch.equal(got, again)
+
+
+@pytest.mark.parametrize("prev,n", [(3000, 1), (3000, 3), (2000, 40), (2048, 200)])
+def test_two_caches_on_two_streams(prev, n):
+    """Steps that run beside each other, pieces and their meeting included, leave the bits of steps one after the other."""
+    folds = [Fold(16, 4, 128, prev + n, seed=s) for s in (1, 50)]
+    data, want, got = [], [], []
+    for f in folds:
+        f.append(prev)
+        data.append([x.cuda() for x in f.chunk(n)])
+        q, k, v = data[-1]
+        want.append(f.cache.step(0, q, k, v, torch.empty_like(q)))
+        f.cache.truncate(0, prev)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in folds]
+    for _ in range(10):
+        for f, (q, k, v), s in zip(folds, data, streams):
+            with torch.cuda.stream(s):
+                got.append(f.cache.step(0, q, k, v, torch.empty_like(q)))
+            f.cache.truncate(0, prev)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, want[i % 2]) for i, x in enumerate(got))
