@@ -4,8 +4,8 @@
 // Rows come in blocks of 64 (block b of a KV head: rows 64 b .. 64 b + 63).  A block whose rows are all there is held as codes, whole numbers from
 // -127 to 127, with one scale for K and one for V:
 //     scale = max(max |x| / 127, 2^-100),   code = x / scale rounded to the nearest whole number (ties to even),
-// both quotients rounded to fp32 first; the row that a code stands for is code * scale.  The floor keeps scale, 1 / scale and scale times the
-// softmax's weights inside the range of fp32; a block below 127 * 2^-100 loses at most 2^-101 an element by it.  Rows of the last,
+// both quotients rounded to fp32 first; the row that a code stands for is code * scale.  The floor keeps scale and 1 / scale inside the range of
+// fp32 (a weight times a small scale may leave it: q_tiny()); a block below 127 * 2^-100 loses at most 2^-101 an element by it.  Rows of the last,
 // incomplete block are held as they came, in bf16, in a ring of two blocks (row r in slot r / 64 % 2), so that what a block is held as
 // does not depend on the chunks that it came in, and the last 64 rows or more can be taken back.  What comes in is made finite: infinities become
 // the largest bf16 number, NaN 0.  (A masked weight is 0, and 0 times infinity is NaN, in rows that do not see the key.)
@@ -151,6 +151,11 @@ __device__ __forceinline__ void q_widen(const quintx4& codes, qbf16x8& lo, qbf16
 
 // What a block's logits are multiplied by; above 0, so that a masked logit, -inf, stays that.
 __device__ __forceinline__ float q_to_log2(float k_scale, float scale_log2e) { return fmaxf(k_scale * scale_log2e, 0x1p-126f); }
+
+// The weights of a block come multiplied by its scale of V.  One as small as this takes them out of fp32's range: what the output
+// loses by that is less than 2^-119 a key, but of the row sum it may be a good part, which is taken from the weights by themselves.  (The scale is the
+// wavefront's; numbers above 0 compare like whole ones.)
+__device__ __forceinline__ bool q_tiny(float v_scale) { return __builtin_amdgcn_readfirstlane((int)__float_as_uint(v_scale)) < (int)__builtin_bit_cast(unsigned, 0x1p-20f); }
 
 // Columns c0 .. c0 + 7 of a query row, rotated if there are angles (the arithmetic of append_rows.h, bit for bit that of a caller who rotates and
 // stores bf16).
