@@ -11,7 +11,7 @@
 // quarters of the values zero: 2048 tokens on 32K keys 1067 us for 996).  The reference m of a row only has to keep the weights
 // inside the range of fp32.  It is the first block's maximum, and is not compared with another's while the row sees all of a block: the sum of a
 // block's weights, needed anyway, tells when it is far behind, and it follows by a power of two.  Logits that rise by more than fp32 holds
-// within one block lose the piece, which the workgroup then does again, with every block's maximum taken.
+// within one block, or values so large that outputs might, lose the piece, which the workgroup then does again, with every block's maximum taken.
 //
 // A turn of a SIMD's two wavefronts, 64 matrix instructions of 32 cycles, takes 1.9 us, 0.58 of what the pipes do alone; the rest is issue: per logit a
 // multiplication, an exponential, an addition and half a rounding, and the widening.  Steps of 32 heads on 8, 128 wide: 256 tokens on 64K keys 270 us
@@ -37,6 +37,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
   constexpr int SLOT = BLOCK * 2;                    // bytes of a block's K, or V, in LDS
   constexpr float kStale = 16.0f;                    // log2 units
   constexpr float kFar = 0x1p60f, kLost = 0x1p100f;  // sums of a lane's weights in a block
+  constexpr float kMost = 0x1p90f;                   // the same times the scale of V: 2^8 of it, in 2^25 blocks, are outputs
   static_assert(T * NT * 16 == 2 * BLOCK && (T == 1 || T == 2), "every thread has the same share of a block");
   __shared__ __attribute__((aligned(16))) unsigned char lds[4 * SLOT];  // K, K, V, V
 
@@ -158,7 +159,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
   };
   // The reference, before a block's exponentials: masks S^T, and moves rows whose maximum asks for it.  Only these move, so that a row's arithmetic never
   // depends on its wave neighbours.
-  auto reference = [&](floatx16 (&s)[2], int b, float to_log2) __attribute__((always_inline)) {
+  auto reference = [&](floatx16 (&s)[2], int b, float to_log2, float v_scale) __attribute__((always_inline)) {
     const int key0 = b * kQBlock;
     if (key0 + kQBlock > vis_first) {  // wave-uniform: some row does not see the whole block
       const int rel = my_vis - key0;
@@ -173,7 +174,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[t][i]);
-    mx = pair_max(mx) * to_log2;
+    mx = __builtin_fmaf(pair_max(mx), to_log2, q_above(v_scale));
     const bool mine = mx > m_run + kStale || (m_run == -INFINITY && mx > -INFINITY);
     if (__any(mine)) {
       const float m2 = mine ? mx : m_run;
@@ -239,6 +240,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) f[i] = operand(i);
     const float inv_v = __builtin_amdgcn_rcpf(v_scale), ref = (m_run == -INFINITY ? 0.f : m_run) - __builtin_amdgcn_logf(v_scale);
+    const float far = fminf(kFar * v_scale, kMost);
     float sum = 0.f, last = 0.f;
     quintx4 pb[2][2], wide;
 #pragma unroll
@@ -274,10 +276,11 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
     }
     load(T - 1, b + 3 - v_of(T - 1));
     l_run = __builtin_fmaf(sum, q_tiny(v_scale) ? 0.f : inv_v, l_run);
-    if (__builtin_expect(__any(!(sum * inv_v < kFar)), 0)) {
-      // Logits far above their row's reference: it follows by a power of two.  Beyond what fp32 holds all is to be done again.
+    if (__builtin_expect(__any(!(sum < far)), 0)) {
+      // Logits far above their row's reference: it follows by a power of two.  Beyond what fp32 holds, of weights or, with V, of outputs, all is to be done
+      // again.
       const float top = pair_max(sum * inv_v);
-      lost |= !(pair_sum(sum * inv_v) < kLost);
+      lost |= !(pair_sum(sum * inv_v) < kLost && pair_sum(sum) < kMost);
       const int by = top >= kFar && top < kLost ? __builtin_amdgcn_frexp_expf(top) : 0;
       const float alpha = __builtin_amdgcn_ldexpf(1.f, -by);
       m_run += (float)by;
@@ -298,7 +301,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
     const floatx2 scale_next = scales[(unsigned)(b + 1)];
     const float to_log2 = q_to_log2(scale.x, p.scale_log2e);
     // every row sees all of the block, and has a reference
-    if (!__all(b * kQBlock + kQBlock <= vis_first && m_run != -INFINITY)) reference(now, b, to_log2);
+    if (!__all(b * kQBlock + kQBlock <= vis_first && m_run != -INFINITY)) reference(now, b, to_log2, scale.y);
     if (__builtin_expect(q_tiny(scale.y), 0)) l_run += plain_sum(now, to_log2);
     turn(now, next, b, to_log2, scale.y);
     scale = scale_next;
@@ -344,7 +347,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
       }
       if (b * kQBlock < vis_last) {
         const float to_log2 = q_to_log2(scale.x, p.scale_log2e);
-        reference(s, b, to_log2);
+        reference(s, b, to_log2, scale.y);
         attend(s, b, to_log2, scale.y);
         if (b + 1 < b_end) logits(s, b + 1);
       }

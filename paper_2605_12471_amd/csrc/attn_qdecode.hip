@@ -11,7 +11,8 @@
 // its share of O the codes times P', rounded to bf16 for the matrix instruction as in the other kernels, and its share of the row sum P' / v,
 // whose factor is taken out of the block's sum.  So neither the queries nor the keys are rounded on the way.  Where v is so small that P' leaves fp32's
 // range (zero rows are held with 2^-100), the row sum's share is summed up from weights without it, a second exponential a logit (three
-// quarters of the values zero: 128K keys 45.8 us for 45.5).  m is the row's maximum, stale by at most 2^16; O, m and l are fp32.
+// quarters of the values zero: 128K keys 45.8 us for 45.5).  m is the row's maximum, stale by at most 2^16, or above it where v is
+// so large that O would leave the range (an infinity among the values is held as the largest number, v = 2^121); O, m and l are fp32.
 //
 // A step whose rows fill no block is one launch: the wavefront that has the incomplete block writes the new rows into it, waits for its own stores and
 // reads them back; nobody else reads them.  (The append as a launch in front takes 4.7 us.)  One token, 32 heads on 8, 128 wide, captured steps: 300
@@ -121,7 +122,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attn_qdecode_kernel(QAttnParam
 #pragma unroll
     for (int t = 0; t < 4; ++t) mx = fmaxf(mx, fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3])));
     mx = pair_max(row16_max(mx));
-    mx *= to_log2;
+    mx = __builtin_fmaf(mx, to_log2, q_above(v_scale));
     // only rows that ask for it move, so a row's arithmetic never depends on its wave neighbours
     const bool mine = mx > m_run + kStale || (m_run == -INFINITY && mx > -INFINITY);
     if (__any(mine)) {

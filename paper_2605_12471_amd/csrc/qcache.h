@@ -157,6 +157,10 @@ __device__ __forceinline__ float q_to_log2(float k_scale, float scale_log2e) { r
 // wavefront's; numbers above 0 compare like whole ones.)
 __device__ __forceinline__ bool q_tiny(float v_scale) { return __builtin_amdgcn_readfirstlane((int)__float_as_uint(v_scale)) < (int)__builtin_bit_cast(unsigned, 0x1p-20f); }
 
+// One as large as 2^64 and more would take the outputs out of it, which are not divided by the row sum before the end: a row's reference then is this much
+// (log2 units) above its maximum.  (Weights of 2^16 above the reference, 127 times a scale and 2^25 blocks of 64 keys: 2^118.)
+__device__ __forceinline__ float q_above(float v_scale) { return fmaxf(__builtin_amdgcn_logf(v_scale) - 64.f, 0.f); }
+
 // Columns c0 .. c0 + 7 of a query row, rotated if there are angles (the arithmetic of append_rows.h, bit for bit that of a caller who rotates and
 // stores bf16).
 template <int D>

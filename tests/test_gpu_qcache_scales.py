@@ -89,3 +89,60 @@ def test_steps_over_blocks_of_tiny_values(d, n, gain):
         q, k, v = f.chunk(n)
         f.step(n, data=(q, k, v * gain if every == 1 else v))
         f.step(1)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [1, 3, 20, 300])
+@pytest.mark.parametrize("block", [0, 2, 5, 9, 14])
+@pytest.mark.parametrize("rise", [0.0, 4.0, 7.0, 10.0, 25.0])
+def test_an_infinity_among_the_values(d, n, block, rise):
+    """A key's value is infinite, taken for the largest number, and its logit `rise` above the others'."""
+    f = Fold(8, 2, d, 1030 + n, seed=block)
+    q, k, v = f.chunk(1030)
+    k[:, :, 0] = 0
+    k[64 * block + 17, :, 0] = 4
+    v[64 * block + 17, :, 3], v[64 * block + 17, 0, 5] = math.inf, -math.inf
+    f.cache.append(0, k.cuda(), v.cuda())
+    f.joined(k, v)
+    q, k, v = f.chunk(n)
+    q = q * 0.1
+    q[:, :, 0], k[:, :, 0] = rise * math.sqrt(d) / 4, 0
+    # (the row's mean has to be some way below the largest number, which the output may else be rounded up from)
+    f.step(n, data=(q, k, v))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("gain", [2.0 ** 30, 2.0 ** 60, 2.0 ** 76, 2.0 ** 80, 2.0 ** 84, 2.0 ** 88, 2.0 ** 118])
+@pytest.mark.parametrize("profile", [lambda j: 20.0 * (j >= 700), lambda j: 30.0 * (j >= 500), lambda j: 38.0 * (j >= 1100), lambda j: 41.0 * (j >= 300), lambda j: 60.0 * (j >= 1100),
+                                     lambda j: 0.4 * j])
+def test_logits_that_jump_where_values_are_large(d, gain, profile):
+    """Weights far above their row's reference, times values far above 1."""
+    hq, hkv, prev, n = 16, 8, 1400, 1000
+    f = Fold(hq, hkv, d, prev + n)
+    g = torch.Generator().manual_seed(d)
+    u = torch.nn.functional.normalize(torch.randn(d, generator=g), dim=0)
+    level = torch.tensor([float(profile(j)) for j in range(prev + n)])
+    k = (0.1 * torch.randn((prev + n, hkv, d), generator=g) + 0.5 * level[:, None, None] * u).to(torch.bfloat16)
+    v = (gain * torch.randn((prev + n, hkv, d), generator=g)).to(torch.bfloat16)
+    q = (0.1 * torch.randn((n, hq, d), generator=g) + 2 * math.sqrt(d) * u).to(torch.bfloat16)
+    f.cache.append(0, k[:prev].cuda(), v[:prev].cuda())
+    f.joined(k[:prev], v[:prev])
+    f.step(n, data=(q, k[prev:], v[prev:]))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [1, 5, 20, 300])
+def test_steps_over_numbers_that_are_hard_to_hold(d, n):
+    """Blocks of V that are zero, tiny, large, with one large element, or not finite, one behind the other."""
+    f = Fold(4, 2, d, 64 * 12 + n + 2)
+    q, k, v = f.chunk(64 * 12)
+    v[64:128] = 0
+    v[128:192] *= 1e-36
+    v[192:256] *= 2.0 ** 100
+    v[256:320, 0, 0] = 1000
+    v[320, 0, 1], v[321, 0, 1], v[322, 0, 1] = math.inf, -math.inf, math.nan
+    v[450:460] *= 2.0 ** 60
+    f.cache.append(0, k.cuda(), v.cuda())
+    f.joined(k, v)
+    f.step(n)
+    f.step(1)
