@@ -341,7 +341,8 @@ int kvfold_measure_peaks(int32_t device, double* mfma_bf16_tflops, double* hbm_r
  *        scale = max(max |x| / 127, 2^-100),  code = round-half-even(x / scale),
  * quotients in fp32; the row that it stands for is code * scale.  Rows of the last, incomplete block are held as they came, in bf16, so that
  * what the cache holds does not depend on the chunks that it was folded in.  Infinities are taken for the largest finite bf16 number of
- * their sign, NaN for 0.  Keys are held rotated, as everywhere.
+ * their sign, NaN for 0; a row's output over such values is finite (but for one that is rounded up from next to the largest number), while
+ * logits beyond fp32's range make it NaN, as in every step.  Keys are held rotated, as everywhere.
  *
  * The configuration is that of a cache, dtype KVFOLD_BF16 (else KVFOLD_ERR_UNSUPPORTED): q, k_new, v_new and out are bf16.  kv_buffer, if given,
  * has kvfold_qcache_bytes_required() bytes.  Errors, streams and threads as for kvfold_cache_t: every error but KVFOLD_ERR_HIP is found before

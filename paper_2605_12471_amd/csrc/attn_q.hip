@@ -157,9 +157,9 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
       if (ks % 2) __builtin_amdgcn_sched_barrier(0);  // (four operands on their way at a time, for want of registers)
     }
   };
-  // The reference, before a block's exponentials: masks S^T, and moves rows whose maximum asks for it.  Only these move, so that a row's arithmetic never
+  // The reference, before a block's exponentials: masks S^T, and moves rows whose maximum, and what they have to be above it, asks for it.  Only these move, so that a row's arithmetic never
   // depends on its wave neighbours.
-  auto reference = [&](floatx16 (&s)[2], int b, float to_log2, float v_scale) __attribute__((always_inline)) {
+  auto reference = [&](floatx16 (&s)[2], int b, float to_log2, float above) __attribute__((always_inline)) {
     const int key0 = b * kQBlock;
     if (key0 + kQBlock > vis_first) {  // wave-uniform: some row does not see the whole block
       const int rel = my_vis - key0;
@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[t][i]);
-    mx = __builtin_fmaf(pair_max(mx), to_log2, q_above(v_scale));
+    mx = __builtin_fmaf(pair_max(mx), to_log2, above);
     const bool mine = mx > m_run + kStale || (m_run == -INFINITY && mx > -INFINITY);
     if (__any(mine)) {
       const float m2 = mine ? mx : m_run;
@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
     const floatx2 scale_next = scales[(unsigned)(b + 1)];
     const float to_log2 = q_to_log2(scale.x, p.scale_log2e);
     // every row sees all of the block, and has a reference
-    if (!__all(b * kQBlock + kQBlock <= vis_first && m_run != -INFINITY)) reference(now, b, to_log2, scale.y);
+    if (!__all(b * kQBlock + kQBlock <= vis_first && m_run != -INFINITY)) reference(now, b, to_log2, q_above(scale.y));
     if (__builtin_expect(q_tiny(scale.y), 0)) l_run += plain_sum(now, to_log2);
     turn(now, next, b, to_log2, scale.y);
     scale = scale_next;
@@ -347,8 +347,9 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
       }
       if (b * kQBlock < vis_last) {
         const float to_log2 = q_to_log2(scale.x, p.scale_log2e);
-        reference(s, b, to_log2, scale.y);
+        reference(s, b, to_log2, b < b_codes ? q_above(scale.y) : again ? kQAboveRows : 0.f);
         attend(s, b, to_log2, scale.y);
+        if (b >= b_codes) lost |= q_large<16>(o);
         if (b + 1 < b_end) logits(s, b + 1);
       }
       scale = scale_of(b + 1);

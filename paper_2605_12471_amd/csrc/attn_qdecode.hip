@@ -208,17 +208,29 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attn_qdecode_kernel(QAttnParam
     }
     qbf16x8 pf[2];
     weights(s, b, 1.f, 1.f, pf);
+    auto outputs = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-      const qbf16x8* at = reinterpret_cast<const qbf16x8*>(vb + (unsigned)(q_v_piece(D, 0, 16 * j) * 32));
+      for (int j = 0; j < J; ++j) {
+        const qbf16x8* at = reinterpret_cast<const qbf16x8*>(vb + (unsigned)(q_v_piece(D, 0, 16 * j) * 32));
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        qbf16x8 v = at[u];
+        for (int u = 0; u < 2; ++u) {
+          qbf16x8 v = at[u];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)  // (places without a row hold anything: 0 times it has to be 0)
-          if (key_mine + 16 * u + 8 * (e >> 2) + (e & 3) >= n) v[e] = (__bf16)0.f;
-        o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[u], o[j], 0, 0, 0);
+          for (int e = 0; e < 8; ++e)  // (places without a row hold anything: 0 times it has to be 0)
+            if (key_mine + 16 * u + 8 * (e >> 2) + (e & 3) >= n) v[e] = (__bf16)0.f;
+          o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[u], o[j], 0, 0, 0);
+        }
       }
+    };
+    outputs();
+    if (__builtin_expect(__any(q_large<4>(o)), 0)) {  // (the wavefront's first results, from weights of at most 1)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) pf[e >> 3][e & 7] = (__bf16)((float)pf[e >> 3][e & 7] * kQLower);
+#pragma unroll
+      for (int j = 0; j < J; ++j) o[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+      outputs();
+      m_run += kQAboveRows;
+      l_run *= kQLower;
     }
   }
 

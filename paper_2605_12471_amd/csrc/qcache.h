@@ -160,6 +160,18 @@ __device__ __forceinline__ bool q_tiny(float v_scale) { return __builtin_amdgcn_
 // One as large as 2^64 and more would take the outputs out of it, which are not divided by the row sum before the end: a row's reference then is this much
 // (log2 units) above its maximum.  (Weights of 2^16 above the reference, 127 times a scale and 2^25 blocks of 64 keys: 2^118.)
 __device__ __forceinline__ float q_above(float v_scale) { return fmaxf(__builtin_amdgcn_logf(v_scale) - 64.f, 0.f); }
+// Rows held as they came may be as large, without a scale that tells.  They are done again with the reference this much above where an output
+// reaches 2^100: 63 numbers of 2^128 and weights of 2^(16 - 32) are 2^118.
+constexpr float kQAboveRows = 32.f, kQLower = 0x1p-32f;  // log2 units, and as a factor
+template <int E, class V, int N>
+__device__ __forceinline__ bool q_large(const V (&o)[N]) {
+  float all = 0.f;
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+#pragma unroll
+    for (int i = 0; i < E; ++i) all = __builtin_fmaf(o[j][i], 0x1p28f, all);
+  return !(fabsf(all) < INFINITY);  // (what is infinite on the way, or NaN, stays so)
+}
 
 // Columns c0 .. c0 + 7 of a query row, rotated if there are angles (the arithmetic of append_rows.h, bit for bit that of a caller who rotates and
 // stores bf16).

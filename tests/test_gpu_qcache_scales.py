@@ -146,3 +146,21 @@ def test_steps_over_numbers_that_are_hard_to_hold(d, n):
     f.joined(k, v)
     f.step(n)
     f.step(1)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [1, 3, 20, 40])
+@pytest.mark.parametrize("prev", [30, 640 + 22, 64 * 40 + 10])
+def test_infinities_in_the_last_block(d, n, prev):
+    """Rows that are not a whole block are held as they came: several of the largest numbers, of either sign, with like weights."""
+    f = Fold(8, 2, d, prev + n + 1, seed=prev)
+    _, k, v = f.chunk(prev)
+    first = prev // 64 * 64
+    v[first + 2:first + 9, :, 3], v[first + 5, 0, 4], v[first + 6, 0, 4], v[first + 7, 1, 5] = math.inf, math.inf, -math.inf, math.nan
+    k[first:, :, 0] = 6.0
+    f.cache.append(0, k.cuda(), v.cuda())
+    f.joined(k, v)
+    q, k, v = f.chunk(n)
+    q[:, :, 0] = 6.0
+    f.step(n, data=(q * 0.5, k, v))
+    f.step(1)
