@@ -6,6 +6,7 @@ fallback path.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import threading
@@ -506,7 +507,8 @@ class KvFoldCache:
         """Enqueue kvfold_cache_evict: per KV head the first n_sink rows, the last n_recent and the heaviest between them, n_keep in all, move
         to the front of this layer or to layer to_layer of the cache `to`.  weights fp32 [Hkv][capacity]; to_weights fp32 [Hkv][capacity of the
         target]; kept int32 [Hkv][n_keep], made here if not given, and returned.  workspace: a uint8 tensor of evict_workspace_bytes(n_keep), else one
-        is made, which takes the memory pool of torch's current stream: with `stream` given, hand in a workspace and kept of that stream."""
+        is made.  What is made here is of the pool of the stream that the call runs on, `stream` or torch's current one; `kept` may be used, behind the
+        call, and let go on either."""
         import torch
         target = self if to is None else to
         if target.handle is None:
@@ -521,8 +523,7 @@ class KvFoldCache:
         else:
             into = None
         if bound is not None and (to is None or into is not None) and type(n_keep) is int and 0 < n_keep and type(weights) is torch.Tensor:
-            rows = torch.empty((self._hkv, n_keep), dtype=torch.int32, device=weights.device) if kept is None else kept
-            space = torch.empty((max(kvfold_evict_workspace_bytes(self.handle, n_keep), 4),), dtype=torch.uint8, device=weights.device) if workspace is None else workspace
+            rows, space = self._evict_memory(weights, n_keep, kept, workspace, stream)
             rc = _native.evict(bound, layer, weights, n_keep, n_sink, n_recent, into, to_layer, to_weights, rows, space, stream)
             if rc == 0:
                 return rows
@@ -531,20 +532,31 @@ class KvFoldCache:
         self._check("weights", weights, (self._hkv, self._capacity), torch.float32)
         if to_weights is not None:
             self._check("to_weights", to_weights, (self._hkv, target._capacity), torch.float32)
-        need = kvfold_evict_workspace_bytes(self.handle, n_keep)
-        if kept is None:
-            kept = torch.empty((self._hkv, max(n_keep, 0)), dtype=torch.int32, device=weights.device)
-        self._check("kept", kept, (self._hkv, n_keep), torch.int32)
-        if workspace is None:
-            workspace = torch.empty((max(need, 4),), dtype=torch.uint8, device=weights.device)
-        else:
+        if workspace is not None:
             self._check("workspace", workspace, (workspace.numel(),), torch.uint8)
+        kept, workspace = self._evict_memory(weights, n_keep, kept, workspace, stream)
+        self._check("kept", kept, (self._hkv, n_keep), torch.int32)
         rc = self._lib.kvfold_cache_evict(self.handle, layer, weights.data_ptr(), n_keep, n_sink, n_recent, None if to is None else to.handle, to_layer,
                                           None if to_weights is None else to_weights.data_ptr(), kept.data_ptr(), workspace.data_ptr(),
                                           workspace.numel(), self._stream(stream))
         if rc:
             raise KvFoldError(rc, "kvfold_cache_evict")
         return kept
+
+    def _evict_memory(self, weights, n_keep, kept, workspace, stream):
+        """kept and workspace, made if they are not given."""
+        import torch
+        if (kept is None or workspace is None) and stream is not None and stream != self._stream(None):
+            made = kept is None
+            with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=self._device)):
+                kept, workspace = self._evict_memory(weights, n_keep, kept, workspace, None)
+            if made and kept.is_cuda:
+                kept.record_stream(torch.cuda.current_stream(self._device))
+        if kept is None:
+            kept = torch.empty((self._hkv, max(n_keep, 0)), dtype=torch.int32, device=weights.device)
+        if workspace is None:
+            workspace = torch.empty((max(kvfold_evict_workspace_bytes(self.handle, n_keep), 4),), dtype=torch.uint8, device=weights.device)
+        return kept, workspace
 
     def evict_workspace_bytes(self, n_keep) -> int:
         return kvfold_evict_workspace_bytes(self.handle, n_keep)

@@ -1,0 +1,81 @@
+"""What the Python binding does around the library's calls, without a GPU: the library, the tensors' checks and torch's streams are stand-ins."""
+import contextlib
+import ctypes
+import types
+
+import pytest
+import torch
+
+import paper_2605_12471_amd as kv
+from paper_2605_12471_amd import binding
+
+HKV, D, CAPACITY = 2, 64, 100
+
+
+class Streams:
+    """torch's streams, by their handles: which is current, and which was at each allocation."""
+
+    def __init__(self, monkeypatch, current=5):
+        self.current, self.made, self.recorded = current, [], []
+        empty = torch.empty
+
+        @contextlib.contextmanager
+        def within(stream):
+            outer, self.current = self.current, stream.cuda_stream
+            yield
+            self.current = outer
+
+        def spy(*shape, **kw):
+            t = empty(*shape, **kw)
+            self.made.append((t.data_ptr(), self.current))
+            return t
+        monkeypatch.setattr(torch, "empty", spy)
+        monkeypatch.setattr(torch.cuda, "stream", within)
+        monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device=None: types.SimpleNamespace(cuda_stream=handle))
+        monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: types.SimpleNamespace(cuda_stream=self.current))
+        monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: self.current, raising=False)
+        monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+        monkeypatch.setattr(torch.Tensor, "is_cuda", True)
+        monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: self.recorded.append((t.data_ptr(), s.cuda_stream)))
+
+    def of(self, address):
+        return [s for a, s in self.made if a == address][-1]
+
+
+def a_cache(monkeypatch, native):
+    """A cache without a library behind it, and the calls of kvfold_cache_evict that it makes: (kept, workspace, stream)."""
+    calls, cache = [], object.__new__(kv.KvFoldCache)
+    cache.handle, cache._device, cache._hq, cache._hkv, cache._d, cache._capacity = ctypes.c_void_p(1), 0, 4, HKV, D, CAPACITY
+    cache._check, cache.close = lambda *a, **k: None, lambda: None
+    monkeypatch.setattr(binding, "kvfold_evict_workspace_bytes", lambda handle, n_keep: 1000)
+
+    def plain(handle, layer, weights, n_keep, n_sink, n_recent, to, to_layer, to_weights, kept, workspace, n_bytes, stream):
+        calls.append((kept, workspace, stream))
+        return 0
+
+    def fast(bound, layer, weights, n_keep, n_sink, n_recent, into, to_layer, to_weights, kept, workspace, stream):
+        calls.append((kept.data_ptr(), workspace.data_ptr(), binding._current_stream() if stream is None else stream))
+        return 0
+    cache._lib = types.SimpleNamespace(kvfold_cache_evict=plain)
+    cache._bound_weights = object() if native else None
+    monkeypatch.setattr(binding, "_native", types.SimpleNamespace(evict=fast))
+    return cache, calls
+
+
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("stream", [None, 5, 7, 0])
+@pytest.mark.parametrize("given", ["nothing", "kept", "workspace", "both"])
+def test_what_an_eviction_takes_is_its_streams_own(monkeypatch, native, stream, given):
+    """Memory of another stream's pool may be given to that stream's next tensor while the eviction still uses it, or be in use there still."""
+    cache, calls = a_cache(monkeypatch, native)
+    kept = torch.zeros((HKV, 10), dtype=torch.int32) if given in ("kept", "both") else None
+    space = torch.zeros(1000, dtype=torch.uint8) if given in ("workspace", "both") else None
+    streams = Streams(monkeypatch)
+    rows = cache.evict(0, torch.zeros((HKV, CAPACITY)), 10, kept=kept, workspace=space, stream=stream)
+    (at_kept, at_space, used), = calls
+    assert used == (5 if stream is None else stream) and streams.current == 5
+    assert rows is kept if kept is not None else rows.data_ptr() == at_kept
+    for mine, address in ((kept, at_kept), (space, at_space)):
+        assert address == mine.data_ptr() if mine is not None else streams.of(address) == used
+    # what is handed out may be used, and let go, on the current stream
+    assert streams.recorded == ([(at_kept, 5)] if kept is None and used != 5 else [])
