@@ -308,14 +308,14 @@ def kvfold_last_hip_error() -> int:
 # ---------------------------------------------------------------------------------------------
 # Convenience wrapper for torch callers (still marshalling only).
 # ---------------------------------------------------------------------------------------------
-def _current_stream() -> int:
-    """Handle of the calling thread's current stream on its current device, what torch.cuda.current_stream().cuda_stream
+def _current_stream(device) -> int:
+    """Handle of the calling thread's current stream on the device, what torch.cuda.current_stream(device).cuda_stream
     is, without the object in between (0.3 us of host time instead of 1.4)."""
     import torch
     try:
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        return torch._C._cuda_getCurrentRawStream(device)
     except AttributeError:
-        return torch.cuda.current_stream().cuda_stream
+        return torch.cuda.current_stream(device).cuda_stream
 
 
 _native = False  # module of csrc/py_step.cpp; None: not there, or built for another torch; False: not looked for yet
@@ -401,7 +401,7 @@ class KvFoldCache:
         self.close()
 
     def _stream(self, stream):
-        return _current_stream() if stream is None else stream
+        return _current_stream(self._device) if stream is None else stream
 
     def _check(self, name, t, shape, dtype=None):
         """Marshalling validation: the kernels trust shapes and element types, so a mismatch must stop here."""

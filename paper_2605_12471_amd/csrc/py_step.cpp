@@ -97,7 +97,7 @@ PyObject* step(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     if (a[7] != Py_None && !(lse = static_cast<float*>(plain(a[7], *c, c10::ScalarType::Float, per_head)))) Py_RETURN_NONE;
     void* stream;
     if (a[8] == Py_None) {
-      stream = c10::hip::getCurrentHIPStream().stream();
+      stream = c10::hip::getCurrentHIPStream((c10::DeviceIndex)c->device).stream();
     } else {
       int64_t s;
       if (!whole_number(a[8], 0, INT64_MAX, &s)) Py_RETURN_NONE;

@@ -33,8 +33,8 @@ class Streams:
         monkeypatch.setattr(torch.cuda, "stream", within)
         monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device=None: types.SimpleNamespace(cuda_stream=handle))
         monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: types.SimpleNamespace(cuda_stream=self.current))
-        monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: self.current, raising=False)
-        monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+        monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: self.current + 100 * device, raising=False)
+        monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)  # (the current device)
         monkeypatch.setattr(torch.Tensor, "is_cuda", True)
         monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: self.recorded.append((t.data_ptr(), s.cuda_stream)))
 
@@ -54,7 +54,7 @@ def a_cache(monkeypatch, native):
         return 0
 
     def fast(bound, layer, weights, n_keep, n_sink, n_recent, into, to_layer, to_weights, kept, workspace, stream):
-        calls.append((kept.data_ptr(), workspace.data_ptr(), binding._current_stream() if stream is None else stream))
+        calls.append((kept.data_ptr(), workspace.data_ptr(), cache._stream(stream)))
         return 0
     cache._lib = types.SimpleNamespace(kvfold_cache_evict=plain)
     cache._bound_weights = object() if native else None
@@ -79,3 +79,24 @@ def test_what_an_eviction_takes_is_its_streams_own(monkeypatch, native, stream, 
         assert address == mine.data_ptr() if mine is not None else streams.of(address) == used
     # what is handed out may be used, and let go, on the current stream
     assert streams.recorded == ([(at_kept, 5)] if kept is None and used != 5 else [])
+
+
+@pytest.mark.parametrize("call", ["step", "noalloc", "rope", "window", "weigh", "evict"])
+def test_the_current_stream_is_that_of_the_caches_device(monkeypatch, call):
+    """A cache on another GPU than the current one: the stream that is current there (100 stands for its device in the handle)."""
+    cache, calls = a_cache(monkeypatch, native=False)
+    Streams(monkeypatch)
+    cache._device, cache._bound, cache.dtype_name, cache.length = 1, None, "bf16", lambda layer: 0
+    names = ("kvfold_step_ex", "kvfold_step_noalloc", "kvfold_step_rope", "kvfold_step_window", "kvfold_cache_weigh", "kvfold_cache_evict")
+    cache._lib = types.SimpleNamespace(**{name: lambda *a: calls.append(a[-1]) for name in names})
+    for name in names:
+        monkeypatch.setattr(binding, name, lambda *a: calls.append(a[-1]))
+    q, k = torch.zeros((3, 4, D), dtype=torch.bfloat16), torch.zeros((3, HKV, D), dtype=torch.bfloat16)
+    angles = (torch.zeros((3, D // 2)), torch.zeros((3, D // 2)))
+    if call == "weigh":
+        cache.weigh(0, q, torch.zeros((4, 3)), torch.zeros((HKV, CAPACITY)))
+    elif call == "evict":
+        cache.evict(0, torch.zeros((HKV, CAPACITY)), 10)
+    else:
+        cache.step(0, q, k, k, torch.zeros_like(q), **{"step": {}, "noalloc": {"noalloc": True}, "rope": {"rope": angles}, "window": {"window": (1, 2)}}[call])
+    assert calls == [105]
