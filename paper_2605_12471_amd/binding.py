@@ -511,6 +511,8 @@ class KvFoldCache:
         call, and let go on either."""
         import torch
         target = self if to is None else to
+        if not isinstance(target, KvFoldCache):
+            raise TypeError(f"to: expected a KvFoldCache, got {type(to).__name__}")
         if target.handle is None:
             raise ValueError("to: the cache is closed")
         bound = self._bound_weights

@@ -100,3 +100,16 @@ def test_the_current_stream_is_that_of_the_caches_device(monkeypatch, call):
     else:
         cache.step(0, q, k, k, torch.zeros_like(q), **{"step": {}, "noalloc": {"noalloc": True}, "rope": {"rope": angles}, "window": {"window": (1, 2)}}[call])
     assert calls == [105]
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_a_target_of_another_kind_is_refused(monkeypatch, native):
+    """Its handle would be taken for a cache's."""
+    cache, calls = a_cache(monkeypatch, native)
+    Streams(monkeypatch)
+    quant = object.__new__(kv.KvFoldQuantCache)
+    quant.handle, quant._bound, quant.close = ctypes.c_void_p(2), None, lambda: None
+    for to in (quant, 7):
+        with pytest.raises(TypeError):
+            cache.evict(0, torch.zeros((HKV, CAPACITY)), 10, to=to)
+    assert not calls
