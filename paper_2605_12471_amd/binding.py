@@ -524,7 +524,7 @@ class KvFoldCache:
                 into = to._bind_weights()
         else:
             into = None
-        if bound is not None and (to is None or into is not None) and type(n_keep) is int and 0 < n_keep and type(weights) is torch.Tensor:
+        if bound is not None and (to is None or into is not None) and type(n_keep) is int and 0 < n_keep <= self._capacity and type(weights) is torch.Tensor:
             rows, space = self._evict_memory(weights, n_keep, kept, workspace, stream)
             rc = _native.evict(bound, layer, weights, n_keep, n_sink, n_recent, into, to_layer, to_weights, rows, space, stream)
             if rc == 0:
@@ -536,8 +536,9 @@ class KvFoldCache:
             self._check("to_weights", to_weights, (self._hkv, target._capacity), torch.float32)
         if workspace is not None:
             self._check("workspace", workspace, (workspace.numel(),), torch.uint8)
-        kept, workspace = self._evict_memory(weights, n_keep, kept, workspace, stream)
-        self._check("kept", kept, (self._hkv, n_keep), torch.int32)
+        if kept is not None:
+            self._check("kept", kept, (self._hkv, n_keep), torch.int32)
+        kept, workspace = self._evict_memory(weights, n_keep if 0 < n_keep <= self._capacity else 0, kept, workspace, stream)
         rc = self._lib.kvfold_cache_evict(self.handle, layer, weights.data_ptr(), n_keep, n_sink, n_recent, None if to is None else to.handle, to_layer,
                                           None if to_weights is None else to_weights.data_ptr(), kept.data_ptr(), workspace.data_ptr(),
                                           workspace.numel(), self._stream(stream))
@@ -555,7 +556,7 @@ class KvFoldCache:
             if made and kept.is_cuda:
                 kept.record_stream(torch.cuda.current_stream(self._device))
         if kept is None:
-            kept = torch.empty((self._hkv, max(n_keep, 0)), dtype=torch.int32, device=weights.device)
+            kept = torch.empty((self._hkv, n_keep), dtype=torch.int32, device=weights.device)
         if workspace is None:
             workspace = torch.empty((max(kvfold_evict_workspace_bytes(self.handle, n_keep), 4),), dtype=torch.uint8, device=weights.device)
         return kept, workspace

@@ -113,3 +113,17 @@ def test_a_target_of_another_kind_is_refused(monkeypatch, native):
         with pytest.raises(TypeError):
             cache.evict(0, torch.zeros((HKV, CAPACITY)), 10, to=to)
     assert not calls
+
+
+def test_more_rows_than_there_are_take_no_memory(monkeypatch):
+    """The library's answer, not that of an allocation of n_keep indices."""
+    for native in (True, False):
+        cache, calls = a_cache(monkeypatch, native)
+        monkeypatch.setattr(binding, "kvfold_evict_workspace_bytes", lambda handle, n_keep: 0 if not 1 <= n_keep <= CAPACITY else 1000)
+        cache._lib.kvfold_cache_evict = lambda *a: -3
+        monkeypatch.setattr(binding._native, "evict", lambda *a: None if a[9].numel() != HKV * a[3] else -3)
+        streams = Streams(monkeypatch)
+        with pytest.raises(kv.KvFoldError) as e:
+            cache.evict(0, torch.zeros((HKV, CAPACITY)), 1 << 40)
+        assert e.value.status == -3
+        monkeypatch.undo()
