@@ -728,12 +728,14 @@ class KvFoldQuantCache:
         """Append rows without attention: k, v [n][Hkv][d], any strides alike of both that are multiples of 8 elements, rows themselves
         contiguous (``KvFoldCache.view(...)[:, :n].transpose(0, 1)``, say)."""
         n = k.shape[0] if k.dim() == 3 else -1
+        strides = []
         for name, t in (("k", k), ("v", v)):
             _expect(name, t, self._bf16, self._device, (n, self._hkv, self._d), contiguous=False)
-            if t.stride() != k.stride() or (n and t.stride(2) != 1):
+            strides.append((t.stride(0) if n > 1 else 0, t.stride(1) if self._hkv > 1 else 0))  # (of one row, or one head, a stride means nothing)
+            if strides[-1] != strides[0] or (n and t.stride(2) != 1):
                 raise ValueError(f"{name}: expected rows of stride 1 and the same strides for k and v, got {t.stride()}")
         cos, sin = self._angles(rope, n)
-        rc = self._lib.kvfold_qcache_append(self.handle, layer, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), n,
+        rc = self._lib.kvfold_qcache_append(self.handle, layer, k.data_ptr(), v.data_ptr(), *strides[0], n,
                                             self.length(layer) if pos_offset is None else pos_offset, cos, sin, self._stream(stream))
         if rc:
             raise KvFoldError(rc, "kvfold_qcache_append")

@@ -127,3 +127,26 @@ def test_more_rows_than_there_are_take_no_memory(monkeypatch):
             cache.evict(0, torch.zeros((HKV, CAPACITY)), 1 << 40)
         assert e.value.status == -3
         monkeypatch.undo()
+
+
+def test_strides_of_dimensions_of_size_one_mean_nothing(monkeypatch):
+    """One row, or one KV head, of any view may be appended; strides that count have to be alike."""
+    calls, cache = [], object.__new__(kv.KvFoldQuantCache)
+    cache.handle, cache._device, cache._hq, cache._hkv, cache._d = ctypes.c_void_p(1), 0, 4, HKV, D
+    cache._bf16, cache._f32, cache.close, cache._stream = torch.bfloat16, torch.float32, lambda: None, lambda s: 0
+    cache._lib = types.SimpleNamespace(kvfold_qcache_append=lambda *a: calls.append(a[4:7]) or 0)
+    monkeypatch.setattr(binding, "_expect", lambda name, t, *a, **k: t.data_ptr())
+    rows = torch.zeros((5, HKV, D), dtype=torch.bfloat16)
+    one = torch.zeros(2000, dtype=torch.bfloat16)
+    cache.append(0, rows[:1], one.as_strided((1, HKV, D), (999, D, 1)), pos_offset=0)
+    cache.append(0, one.as_strided((1, HKV, D), (999, D, 1)), rows[:1], pos_offset=0)
+    cache._hkv = 1
+    cache.append(0, rows[:, :1], one.as_strided((5, 1, D), (HKV * D, 7, 1)), pos_offset=0)
+    cache.append(0, one.as_strided((1, 1, D), (5, 7, 1)), rows[:1, :1], pos_offset=0)
+    assert [a[2] for a in calls] == [1, 1, 5, 1] and calls[2][0] == HKV * D
+    assert all(s >= 0 and s % 8 == 0 for a in calls for s in a[:2]) and calls[0][1] == calls[1][1] == D
+    cache._hkv = HKV
+    for k, v in ((rows[:2], one.as_strided((2, HKV, D), (3 * D, D, 1))), (rows[:1], one.as_strided((1, HKV, D), (HKV * D, 2 * D, 1))),
+                 (one.as_strided((1, HKV, D), (HKV * D, D, 2)), one.as_strided((1, HKV, D), (HKV * D, D, 2)))):
+        with pytest.raises(ValueError):
+            cache.append(0, k, v, pos_offset=0)
