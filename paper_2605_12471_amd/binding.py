@@ -612,7 +612,8 @@ class KvFoldCache:
         return n, a, t, m
 
     def view(self, layer=0):
-        """(K, V) device tensors [Hkv][capacity][d] aliasing the cache rows of ``layer`` (no copy)."""
+        """(K, V) device tensors [Hkv][capacity][d] aliasing the cache rows of ``layer`` (no copy).  They keep the cache from being collected; ``close()``
+        frees their memory all the same."""
         import torch
         rc, k, v, rs, hs = kvfold_cache_view(self.handle, layer)
         if rc:
@@ -625,7 +626,9 @@ class KvFoldCache:
                 __cuda_array_interface__ = {"shape": (c.n_kv_heads, c.capacity_tokens, c.head_dim),
                                             "typestr": "<f4" if es == 4 else "<i2", "data": (ptr, False),
                                             "version": 3}
-            t = torch.as_tensor(_Holder(), device=f"cuda:{c.device}")
+            holder = _Holder()
+            holder.owner = self  # (torch holds on to the holder as long as there is a tensor on the memory)
+            t = torch.as_tensor(holder, device=f"cuda:{c.device}")
             return t if es == 4 else t.view(torch.bfloat16)
 
         return wrap(k), wrap(v)

@@ -25,3 +25,24 @@ def test_rows_of_odd_strides_that_mean_nothing(hkv, n, at):
     cache.read(0, 0, *got)
     for x in got:
         assert np.array_equal(x.cpu().numpy(), R.held(k.float().numpy()).astype(np.float32))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_view_keeps_its_cache(dtype):
+    cache = kv.KvFoldCache(1, 2, 2, 64, 8, 50, dtype)
+    k, v = cache.view(0)
+    known = weakref.ref(cache)
+    del cache
+    gc.collect()
+    assert known() is not None          # (nothing is read before this is known)
+    k.fill_(2.0)
+    part = k[1, 3:5]
+    del k, v
+    gc.collect()
+    assert known() is not None and (part == 2).all()
+    gc.disable()
+    try:
+        del part
+        assert known() is None          # (at once, not when rubbish is next collected)
+    finally:
+        gc.enable()
