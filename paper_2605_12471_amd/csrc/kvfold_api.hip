@@ -673,6 +673,8 @@ int kvfold_cache_evict(kvfold_cache_t* c, int layer, const float* weights, int64
       ok = ok && (own_rows || own_weights || apart(out[i].at, out[i].bytes, in[j].at, in[j].bytes));
     }
     for (int j = 0; j < i; ++j) ok = ok && (!out[j].bytes || apart(out[i].at, out[i].bytes, out[j].at, out[j].bytes));
+    // (nor in other layers' rows, of either cache)
+    if (i < 3) ok = ok && apart(out[i].at, out[i].bytes, c->kv, c->kv_bytes) && apart(out[i].at, out[i].bytes, to->kv, to->kv_bytes);
   }
   if (!ok) return KVFOLD_ERR_INVALID_ARG;
 
