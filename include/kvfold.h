@@ -368,7 +368,7 @@ int kvfold_qcache_step(kvfold_qcache_t* cache, int layer, const void* q, const v
 /*
  * Append without attention, any number of tokens that fits: to carry on in 8 bits what another cache holds, or to restore a fold.
  *   k, v  device, bf16, 16-byte aligned: row t of KV head g begins token_stride * t + head_stride * g elements behind the pointer, both
- *         multiples of 8 (kvfold_cache_view's row and head strides, say, or Hkv * d and d for [n][Hkv][d])
+ *         multiples of 8 (kvfold_cache_view's row and head strides, say, or Hkv * d and d for [n][Hkv][d]); not in the cache's storage
  *   rope_cos, rope_sin  NULL, or the angles by which the K rows are rotated on their way, as for kvfold_step_rope
  */
 int kvfold_qcache_append(kvfold_qcache_t* cache, int layer, const void* k, const void* v, int64_t token_stride, int64_t head_stride,
@@ -376,7 +376,7 @@ int kvfold_qcache_append(kvfold_qcache_t* cache, int layer, const void* k, const
 
 /*
  * Rows [first, first + n_tokens) of `layer` as the numbers they stand for, code * scale (or the bf16 row) in fp32.
- *   k_out, v_out  device, 16-byte aligned, [n_tokens][Hkv][d]; either may be NULL
+ *   k_out, v_out  device, 16-byte aligned, [n_tokens][Hkv][d]; either may be NULL; apart from one another and from the cache's storage
  * KVFOLD_ERR_POSITION for rows that the layer does not have.
  */
 int kvfold_qcache_read(kvfold_qcache_t* cache, int layer, int64_t first, int64_t n_tokens, float* k_out, float* v_out, void* stream);

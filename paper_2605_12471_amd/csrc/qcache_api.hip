@@ -170,6 +170,8 @@ int kvfold_qcache_append(kvfold_qcache_t* c, int layer, const void* k, const voi
   if (pos_offset != len.len) return KVFOLD_ERR_POSITION;
   if (n_tokens > f.capacity_tokens - len.len) return KVFOLD_ERR_CAPACITY;
   if (n_tokens == 0) return KVFOLD_OK;
+  const size_t extent = ((size_t)(n_tokens - 1) * (size_t)token_stride + (size_t)(f.n_kv_heads - 1) * (size_t)head_stride + (size_t)f.head_dim) * 2;
+  if (!apart(c->store, c->bytes(), k, extent) || !apart(c->store, c->bytes(), v, extent)) return KVFOLD_ERR_INVALID_ARG;
   DeviceGuard guard(f.device);
   if (guard.err != hipSuccess) return hip_fail(guard.err);
   const hipError_t e = append(c, layer, k, v, token_stride, head_stride, n_tokens, rope_cos, rope_sin, static_cast<hipStream_t>(stream));
@@ -267,6 +269,10 @@ int kvfold_qcache_read(kvfold_qcache_t* c, int layer, int64_t first, int64_t n_t
   const int64_t len = c->len[(size_t)layer].len;
   if (first > len || n_tokens > len - first) return KVFOLD_ERR_POSITION;
   if (n_tokens == 0 || (!k_out && !v_out)) return KVFOLD_OK;
+  const size_t bytes = (size_t)n_tokens * c->cfg.n_kv_heads * c->cfg.head_dim * sizeof(float);
+  if ((k_out && !apart(c->store, c->bytes(), k_out, bytes)) || (v_out && !apart(c->store, c->bytes(), v_out, bytes)) ||
+      (k_out && v_out && !apart(k_out, bytes, v_out, bytes)))
+    return KVFOLD_ERR_INVALID_ARG;
   DeviceGuard guard(c->cfg.device);
   if (guard.err != hipSuccess) return hip_fail(guard.err);
   QReadParams p;
