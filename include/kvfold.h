@@ -403,7 +403,7 @@ int kvfold_qcache_truncate(kvfold_qcache_t* cache, int layer, int64_t new_len);
  * fewer keys).  The weights of a KV head add up to n_tokens * Hq / Hkv.
  *   q        device, [n_tokens][Hq][d], 1 <= n_tokens <= cfg.chunk_tokens
  *   rope_cos, rope_sin  NULL, or the angles of the rows if q is unrotated, as for kvfold_step_rope
- *   lse      device, [Hq][n_tokens]; a row whose lse is -inf counts for nothing
+ *   lse      device, [Hq][n_tokens]; a row whose lse is -inf counts for nothing, whatever its q is
  *   weights  device, [Hkv][capacity_tokens] float.  add = 0: entries [0, length) are set, add = 1: added to (which needs entries that begin
  *            at zero); entries behind are left alone.  Apart from all inputs, else KVFOLD_ERR_INVALID_ARG.
  * KVFOLD_ERR_POSITION if the layer has fewer than n_tokens rows.  The sums are fp32; the same call gives the same bits.

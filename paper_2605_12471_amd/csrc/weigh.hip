@@ -13,7 +13,8 @@
 // Few rows (at most 16 a KV head) are bound by reading the keys: the wavefronts take 64 keys at a time straight into registers, on the 16x16x32
 // shapes, whole 64-byte pieces of rows an instruction.
 //
-// A row whose log-sum-exp is -inf gave no weight to any key.
+// A row whose log-sum-exp is -inf gave no weight to any key, whatever its query is: it sees no key.  (Many rows, bf16: its sums begin with -inf, which a
+// query that is not finite makes NaN.  A wavefront with such a weight goes through its rows again, straight from memory, with zeros for these queries.)
 #include "append_rows.h"
 #include "qcache.h"
 #include "wave_ops.h"
@@ -144,6 +145,25 @@ __global__ void __launch_bounds__(64 * KW * RW, 2) weigh_bf16_kernel(WeighParams
     mask(u_last);
     add_up();
   }
+  if (__builtin_expect(__any(sum != sum), 0)) {
+    sum = 0.f;
+#pragma unroll 1
+    for (int u = u_begin + rw; u < units; u += RW) {
+      const int row = u * 32 + c32 < rows ? u * 32 + c32 : rows - 1, tok = (int)quot((unsigned)row, p.by_group);
+      const __bf16* q_row = q_all + (uint64_t)(unsigned)(row + tok * (p.n_q_heads - p.group)) * D;
+      const bool off = lse_log2(p, g, row, rows) == INFINITY;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = -lse_log2(p, g, u * 32 + 8 * (i >> 2) + 4 * h + (i & 3), rows) * to_logit;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        qbf16x8 q = q_query<D>(q_row, 16 * ks + 8 * h, p.rope_cos ? p.rope_cos + (int64_t)tok * (D / 2) : nullptr, p.rope_cos ? p.rope_sin + (int64_t)tok * (D / 2) : nullptr);
+        if (off) q = qbf16x8{};
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, kf[ks], s, 0, 0, 0);
+      }
+      mask(u);
+      add_up();
+    }
+  }
   sum = pair_sum(sum);
   if constexpr (RW > 1) {
     float* part = reinterpret_cast<float*>(q_lds);  // (behind the last barrier)
@@ -185,7 +205,7 @@ __global__ void __launch_bounds__(256, 4) weigh_few_bf16_kernel(WeighParams p) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     m[e] = lse_log2(p, g, 4 * kg + e, rows);
-    at[e] = prev + (int)quot((unsigned)(4 * kg + e), p.by_group);
+    at[e] = m[e] == INFINITY ? -1 : prev + (int)quot((unsigned)(4 * kg + e), p.by_group);
   }
   for (int strip = blockIdx.x * 4 + (tid >> 6); strip * 64 < p.len; strip += gridDim.x * 4) {
     qbf16x8 kf[4][KS];
@@ -239,7 +259,7 @@ __global__ void __launch_bounds__(64 * KW * RW, 2) weigh_f32_kernel(WeighParams 
     for (int i = 0; i < CH; ++i) q[i] = *reinterpret_cast<const floatx4*>(q_row + 8 * i + 4 * h);
     // lane r of the wavefront's first 32 finds row r's log-sum-exp, and the last key that it sees
     const float lse = lse_log2(p, g, u * 32 + c32, rows);
-    const int last = prev + (int)quot((unsigned)(u * 32 + c32), p.by_group);
+    const int last = lse == INFINITY ? -1 : prev + (int)quot((unsigned)(u * 32 + c32), p.by_group);
     if (p.rope_cos) {
 #pragma unroll
       for (int i = 0; i < CH / 2; ++i) {  // (a lane holds both elements of its pairs)
