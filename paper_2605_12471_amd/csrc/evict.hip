@@ -313,10 +313,9 @@ __global__ void __launch_bounds__(256) evict_move_kernel(EvictParams p) {
     if (tid == 0) {
       uint32_t* read = p.workspace + p.ws.read + (int64_t)g * p.ws.chunks;
       __hip_atomic_store(read + chunk, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      // the kept rows that lie in places row0 .. row0 + n - 1: their numbers, and the chunks that these are in
       const uint32_t* before = p.workspace + p.ws.before + (int64_t)g * (p.ws.chunks + 1) + chunk;
-      const uint32_t first = before[0], end = before[1];
-      for (int other = (int)(first / kEvictRows); other < chunk && (uint32_t)other * kEvictRows < end; ++other)
+      const EvictWaits others = evict_waits(before[0], before[1], chunk);
+      for (int other = others.from; other < others.to; ++other)
         while (__hip_atomic_load(read + other, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 0) __builtin_amdgcn_s_sleep(1);
     }
     __syncthreads();

@@ -51,6 +51,18 @@ inline QLayout q_layout(const kvfold_config_t& c) {
   return l;
 }
 
+// Who writes the ring when rows [prev, prev + n) are appended, a workgroup a block (and KV head, K or V).  The ring takes the rows of the last two
+// blocks.  Whose slot the first block's earlier rows lie in, if it has any, is written by the first block's workgroup, once it has read them.
+struct QRingWriters {
+  int64_t first, last;  // the blocks that get rows
+  bool earlier;         // the first one has rows already
+  KVFOLD_HD QRingWriters(int64_t prev, int64_t n) : first(prev / kQBlock), last((prev + n - 1) / kQBlock), earlier(prev % kQBlock != 0) {}
+  // The block's workgroup writes its new rows, before all else.
+  KVFOLD_HD bool itself(int64_t block) const { return block + kQRing > last && !(earlier && block != first && (block - first) % kQRing == 0); }
+  // The block whose new rows the first block's workgroup writes at its end; first: none
+  KVFOLD_HD int64_t taken_over() const { return earlier ? last - (last - first) % kQRing : first; }
+};
+
 // What the host knows of a layer.  Rows [ring_from, len) are in the ring, but for those of blocks that begin before ring_from.
 struct QLength {
   int64_t len = 0, ring_from = 0;

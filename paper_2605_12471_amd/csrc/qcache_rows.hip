@@ -93,21 +93,19 @@ __device__ __forceinline__ void append_block(const QAppendParams& p, int g) {
   constexpr int N = kQBlock * D / 16, T = N / kThreads;  // pieces, and those of a thread
   __shared__ float wave_max[kThreads / 64];
   const int tid = threadIdx.x;
-  const int64_t first = p.len_prev / kQBlock, end = p.len_prev + p.n, last = (end - 1) / kQBlock, block = first + blockIdx.x;
+  const QRingWriters writers(p.len_prev, p.n);
+  const int64_t end = p.len_prev + p.n, block = writers.first + blockIdx.x;
   __bf16* ring = p.to.ring[V] + (int64_t)g * (kQRing * kQBlock * D);
   Piece<D, V> q[T];
 #pragma unroll
   for (int j = 0; j < T; ++j) q[j] = piece_in<D, V>(p, block, g, tid + j * kThreads);
-  // The ring takes the rows of the last two blocks.  Whose slot the first block's earlier rows lie in, if it has any, is written by the first block's
-  // workgroup, once it has read them.
-  const bool earlier = p.len_prev % kQBlock != 0, later = earlier && block != first && (block - first) % kQRing == 0;
-  if (block + kQRing > last && !later) {
+  if (writers.itself(block)) {
 #pragma unroll
     for (int j = 0; j < T; ++j) to_ring<D, V>(ring + (block % kQRing) * (kQBlock * D), tid + j * kThreads, q[j]);
   }
   const bool whole = (block + 1) * kQBlock <= end;
   if (whole) {
-    if (block == first && earlier) {
+    if (block == writers.first && writers.earlier) {
       const unsigned short* slot = reinterpret_cast<const unsigned short*>(ring) + (block % kQRing) * (kQBlock * D);
 #pragma unroll
       for (int j = 0; j < T; ++j) {
@@ -151,8 +149,8 @@ __device__ __forceinline__ void append_block(const QAppendParams& p, int g) {
     }
   }
   // The block whose rows take the place of the first block's in the ring
-  const int64_t over = last - (last - first) % kQRing;
-  if (block == first && earlier && over > first) {
+  const int64_t over = writers.taken_over();
+  if (block == writers.first && over > block) {
     __syncthreads();  // (the block's earlier rows have been read: their values went into the codes' scale)
 #pragma unroll 1
     for (int j = 0; j < T; ++j) to_ring<D, V>(ring + (over % kQRing) * (kQBlock * D), tid + j * kThreads, piece_in<D, V>(p, over, g, tid + j * kThreads));

@@ -3,6 +3,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "kvfold_consts.h"
+
 namespace kvfold {
 
 constexpr int kEvictRows = 64;     // rows that a workgroup moves
@@ -31,6 +33,16 @@ inline EvictLayout evict_layout(int64_t n_kv_heads, int64_t n_keep, int64_t capa
   l.state = l.more + (size_t)(n_kv_heads * l.pieces);
   l.words = l.state + 4 * (size_t)n_kv_heads;
   return l;
+}
+
+// The chunks [from, to) that a chunk, moved in place, waits for: in front of it, with kept rows that lie where it writes.  front, behind: how many kept rows
+// lie before its first place and before the place behind its last.
+struct EvictWaits {
+  int from, to;
+};
+KVFOLD_HD EvictWaits evict_waits(uint32_t front, uint32_t behind, int chunk) {
+  const int end = (int)((behind + kEvictRows - 1) / kEvictRows);
+  return EvictWaits{(int)(front / kEvictRows), end < chunk ? end : chunk};
 }
 
 }  // namespace kvfold
