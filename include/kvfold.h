@@ -385,9 +385,11 @@ int kvfold_qcache_read(kvfold_qcache_t* cache, int layer, int64_t first, int64_t
 int64_t kvfold_qcache_length(const kvfold_qcache_t* cache, int layer);
 
 /*
- * Rewind `layer` (-1 = every layer) to `new_len` rows.  An incomplete block's rows have to be there in bf16: those of the last two blocks that
- * rows were appended to are, so that at least the last 64 rows can be taken back to any place (and again, to where these two blocks begin);
- * further back new_len must be a multiple of 64.  Else, or beyond the current length, KVFOLD_ERR_POSITION and nothing changes.  Host-only.
+ * Rewind `layer` (-1 = every layer) to `new_len` rows, at most its length: to a multiple of 64, or to any place from R on, where an incomplete block's
+ * rows are there in bf16.  An append sets R to the beginning of the block before the last one that has rows, unless R lies behind that already (at
+ * first R = 0); a rewind to a multiple of 64 in front of R sets R to that.  So behind an append the last 64 rows can be taken back to any place, but
+ * for rows that such a rewind has left as codes: 300 rows, R = 192; rewound to 128 and 10 rows appended, 128 to 138 and multiples of 64.
+ * Else KVFOLD_ERR_POSITION and nothing changes.  Host-only.
  */
 int kvfold_qcache_truncate(kvfold_qcache_t* cache, int layer, int64_t new_len);
 

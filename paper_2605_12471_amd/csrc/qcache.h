@@ -7,7 +7,7 @@
 // both quotients rounded to fp32 first; the row that a code stands for is code * scale.  The floor keeps scale and 1 / scale inside the range of
 // fp32 (a weight times a small scale may leave it: q_tiny()); a block below 127 * 2^-100 loses at most 2^-101 an element by it.  Rows of the last,
 // incomplete block are held as they came, in bf16, in a ring of two blocks (row r in slot r / 64 % 2), so that what a block is held as
-// does not depend on the chunks that it came in, and the last 64 rows or more can be taken back.  What comes in is made finite: infinities become
+// does not depend on the chunks that it came in, and behind an append the last 64 rows can be taken back, but for those that a rewind has left as codes (QLength).  What comes in is made finite: infinities become
 // the largest bf16 number, NaN 0.  (A masked weight is 0, and 0 times infinity is NaN, in rows that do not see the key.)
 //
 // A block lies as the matrix instructions want it, in pieces of 16 elements, codes (16 bytes) or bf16 (32 bytes) alike:
