@@ -408,7 +408,8 @@ int kvfold_qcache_truncate(kvfold_qcache_t* cache, int layer, int64_t new_len);
  *   lse      device, [Hq][n_tokens]; a row whose lse is -inf counts for nothing, whatever its q is
  *   weights  device, [Hkv][capacity_tokens] float.  add = 0: entries [0, length) are set, add = 1: added to (which needs entries that begin
  *            at zero); entries behind are left alone.  Apart from all inputs, else KVFOLD_ERR_INVALID_ARG.
- * KVFOLD_ERR_POSITION if the layer has fewer than n_tokens rows.  The sums are fp32; the same call gives the same bits.
+ * KVFOLD_ERR_POSITION if the layer has fewer than n_tokens rows.  Products, exponents and sums are fp32, in bf16 with more than 16 rows a KV head begun
+ * with -lse / scale: a weight is good to a few 2^-24 of |lse| and of its logit's terms.  The same call gives the same bits.
  */
 int kvfold_cache_weigh(kvfold_cache_t* cache, int layer, const void* q, int32_t n_tokens, const float* rope_cos, const float* rope_sin,
                        const float* lse, float* weights, int32_t add, void* stream);

@@ -13,10 +13,11 @@
 // block's weights, needed anyway, tells when it is far behind, and it follows by a power of two.  Logits that rise by more than fp32 holds
 // within one block, or values so large that outputs might, lose the piece, which the workgroup then does again, with every block's maximum taken.
 //
-// A turn of a SIMD's two wavefronts, 64 matrix instructions of 32 cycles, takes 1.9 us, 0.58 of what the pipes do alone; the rest is issue: per logit a
-// multiplication, an exponential, an addition and half a rounding, and the widening.  Steps of 32 heads on 8, 128 wide: 256 tokens on 64K keys 270 us
-// (1.02 PFLOP/s), 2048 on 32K 1030 us (1.10); 64 wide, 1000 on 8K, where a logit has half the products, 102 us (0.69).  Codes three turns ahead
-// by copies to LDS took as long (1033 us), and so did codes of one place for every block: it is not the memory that is waited for.
+// A turn of a SIMD's two wavefronts, 64 matrix instructions of 32 cycles, takes 1.9 us, 0.59 of what the pipes do alone; the rest is issue, 5.8 vector
+// instructions beside each: per logit a multiplication, an exponential, an addition and half a rounding, and the widening.  Steps of 32 heads on 8, 128
+// wide: 256 tokens on 64K keys 269 us (1.02 PFLOP/s), 2048 on 32K 1008 us (1.12); 64 wide, 1000 on 8K, where a logit has half the products, 100 us
+// (0.71).  Codes three turns ahead by copies to LDS took as long as without, and so did codes of one place for every block: it is not the memory
+// that is waited for.
 #include "qcache.h"
 #include "wave_ops.h"
 
@@ -157,8 +158,9 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_q_kernel(QAttnParams qp) {
       if (ks % 2) __builtin_amdgcn_sched_barrier(0);  // (four operands on their way at a time, for want of registers)
     }
   };
-  // The reference, before a block's exponentials: masks S^T, and moves rows whose maximum, and what they have to be above it, asks for it.  Only these move, so that a row's arithmetic never
-  // depends on its wave neighbours.
+  // The reference, before a block's exponentials: masks S^T, and moves rows whose maximum, and what they have to be above it, asks for it.  (Whether it is looked at
+  // depends on the wavefront's other rows, and whether a piece is done again on the workgroup's: a row among other rows may be rounded otherwise, the
+  // same call gives the same bits.)
   auto reference = [&](floatx16 (&s)[2], int b, float to_log2, float above) __attribute__((always_inline)) {
     const int key0 = b * kQBlock;
     if (key0 + kQBlock > vis_first) {  // wave-uniform: some row does not see the whole block

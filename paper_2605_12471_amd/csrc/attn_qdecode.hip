@@ -16,7 +16,7 @@
 //
 // A step whose rows fill no block is one launch: the wavefront that has the incomplete block writes the new rows into it, waits for its own stores and
 // reads them back; nobody else reads them.  (The append as a launch in front takes 4.7 us.)  One token, 32 heads on 8, 128 wide, captured steps: 300
-// keys 6.7 us, 4187 7.5, 16K 10.1, 128K 46 (268 MB of codes, 5.8 TB/s).
+// keys 6.7 us, 4187 7.6, 16K 11.1, 128K 46 (268 MB of codes, 5.8 TB/s).
 #include "meet.h"
 #include "qcache.h"
 

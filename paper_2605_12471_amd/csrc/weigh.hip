@@ -5,9 +5,11 @@
 // S = Q K^T with the queries as the matrix instruction's rows: a lane holds the logits of one key, which it adds up without a word to other lanes
 // until the end.  The keys stay in registers and the queries stream past, through LDS, units of 32 packed rows at a time, two buffers, one
 // barrier.  What a logit's sum begins with is the row's -lse / (scale log2 e), so that a multiplication, an exponential and an addition are
-// all that is left to do to it.  Bound by issue: a 32x32x16 matrix instruction keeps its pipe busy for 32 cycles, 128 wide 16 a logit and lane, and the vector
-// port for 16 of them; a logit's own instructions take it for 16 more, of which no more than half go beside matrix instructions.  256 tokens on
-// 64K keys, 28 heads on 4, 158 us, 762 TFLOP/s: matrix pipes 0.29 busy, the vector port 0.72 of the time that a CU has work.  Two or three blocks of
+// all that is left to do to it; the product's sums are rounded at that size for it, 5.8e-7 of a weight (2-norm; 9e-8 where it is added last).  Bound by
+// issue: a 32x32x16 matrix instruction keeps its pipe busy for 32 cycles, 128 wide 16 a logit and lane, and the vector port for 16 of them; a logit's own
+// instructions take it for 16 more, of which no more than half go beside matrix instructions, and of the 11 vector instructions beside each of these
+// a third finds the rows (ten for a piece of a query, fourteen for a log-sum-exp).  256 tokens on 64K keys, 28 heads on 4, 158 us, 762 TFLOP/s: matrix
+// pipes 0.33 busy, the vector port 0.72 of the time that a CU has work.  Two or three blocks of
 // 32 keys a wavefront (fewer wavefronts a SIMD), queries two stages ahead, and a schedule written out gained nothing.
 //
 // Few rows (at most 16 a KV head) are bound by reading the keys: the wavefronts take 64 keys at a time straight into registers, on the 16x16x32
