@@ -170,7 +170,8 @@ __device__ __forceinline__ float q_to_log2(float k_scale, float scale_log2e) { r
 __device__ __forceinline__ bool q_tiny(float v_scale) { return __builtin_amdgcn_readfirstlane((int)__float_as_uint(v_scale)) < (int)__builtin_bit_cast(unsigned, 0x1p-20f); }
 
 // One as large as 2^64 and more would take the outputs out of it, which are not divided by the row sum before the end: a row's reference then is this much
-// (log2 units) above its maximum.  (Weights of 2^16 above the reference, 127 times a scale and 2^25 blocks of 64 keys: 2^118.)
+// (log2 units) above its maximum.  (Weights of 2^16 above the reference, 127 times a scale and 2^25 blocks of 64 keys: 2^118.
+// Such a row's weights and outputs are held up to 2^57 smaller for it: weights below 2^-69 of the largest are lost, and outputs below 2^-69.)
 __device__ __forceinline__ float q_above(float v_scale) { return fmaxf(__builtin_amdgcn_logf(v_scale) - 64.f, 0.f); }
 // Rows held as they came may be as large, without a scale that tells.  They are done again with the reference this much above where an output
 // reaches 2^100: 63 numbers of 2^128 and weights of 2^(16 - 32) are 2^118.
