@@ -360,7 +360,7 @@ int kvfold_qcache_destroy(kvfold_qcache_t* cache);
  * One fold step on one layer, n_tokens in [1, cfg.chunk_tokens]: append the chunk's rows, then let query row i attend to the rows
  * j <= pos_offset + i as the cache holds them after the append.  q, k_new, v_new, out, lse as for kvfold_step_ex; rope_cos and rope_sin as for
  * kvfold_step_rope, or both NULL: q and k_new are used as given.  out may lie on q, k_new or v_new (in q's very place); any other
- * overlap of out or lse with q, the angles, the cache's storage or one another is KVFOLD_ERR_INVALID_ARG.
+ * overlap of out or lse with q, the angles, the cache's storage or one another, and q, k_new or v_new in that storage, is KVFOLD_ERR_INVALID_ARG.
  */
 int kvfold_qcache_step(kvfold_qcache_t* cache, int layer, const void* q, const void* k_new, const void* v_new, int32_t n_tokens,
                        int64_t pos_offset, const float* rope_cos, const float* rope_sin, void* out, float* lse, void* stream);

@@ -198,6 +198,9 @@ int kvfold_qcache_step(kvfold_qcache_t* c, int layer, const void* q, const void*
   for (const float* a : {rope_cos, rope_sin})
     if (a) ok = ok && apart(a, angles, out, wide) && (!lse || apart(a, angles, lse, sums));
   ok = ok && apart(c->store, c->bytes(), out, wide) && (!lse || apart(c->store, c->bytes(), lse, sums));
+  // (and the cache is written while the inputs are read)
+  const size_t narrow = (size_t)n_tokens * f.n_kv_heads * f.head_dim * 2;
+  ok = ok && apart(c->store, c->bytes(), q, wide) && apart(c->store, c->bytes(), k_new, narrow) && apart(c->store, c->bytes(), v_new, narrow);
   if (!ok) return KVFOLD_ERR_INVALID_ARG;
 
   DeviceGuard guard(f.device);
@@ -234,7 +237,6 @@ int kvfold_qcache_step(kvfold_qcache_t* c, int layer, const void* q, const void*
 
   // Rows that fill no block are appended by the attention kernel, where one workgroup alone reads a head's last block and its results lie apart from them:
   // these are stored while other heads' rows are still read.  37 tokens on 32K keys 47.5 us for 51, 32 on 4187 24.1 for 27.
-  const size_t narrow = (size_t)n_tokens * f.n_kv_heads * f.head_dim * 2;
   bool inside = pl.wgs_per_head == 1 && len.len / kQBlock == (len.len + n_tokens) / kQBlock;
   for (const void* rows : {k_new, v_new}) inside = inside && apart(rows, narrow, out, wide) && (!lse || apart(rows, narrow, lse, sums));
   p.k_new = inside ? static_cast<const __bf16*>(k_new) : nullptr;

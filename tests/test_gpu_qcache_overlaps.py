@@ -29,7 +29,13 @@ def test_refused_before_anything_is_enqueued():
         assert kv.kvfold_qcache_append(h, 1, a, b, HKV * D, D, 10, 0) == -1
     # rows [Hkv][capacity][d] whose last head is the one that lies there
     assert kv.kvfold_qcache_append(h, 1, base - 4096, rows.data_ptr(), D, 2048, 1, 0) == -1
+    # a step's inputs
+    q, kn, vn, o = (torch.ones((4, n, D), device="cuda", dtype=torch.bfloat16) for n in (4, HKV, HKV, 4))
+    for name, at in (("q", base), ("k", base + need - 512), ("v", base + need // 256 // 2 * 256)):
+        place = {"q": q.data_ptr(), "k": kn.data_ptr(), "v": vn.data_ptr(), name: at}
+        assert kv.kvfold_qcache_step(h, 0, place["q"], place["k"], place["v"], 4, 200, None, None, o.data_ptr()) == -1
     torch.cuda.synchronize()
+    assert (o == 1).all() and kv.kvfold_qcache_length(h, 0) == 200
     assert torch.equal(buf, held) and kv.kvfold_qcache_length(h, 1) == 0 and not out.any()
     assert kv.kvfold_qcache_read(h, 0, 0, 200, k, v) == 0 and kv.kvfold_qcache_read(h, 0, 0, 0, base, base) == 0
     torch.cuda.synchronize()
