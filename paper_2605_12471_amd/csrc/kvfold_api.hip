@@ -620,7 +620,7 @@ int kvfold_cache_weigh(kvfold_cache_t* c, int layer, const void* q, int32_t n_to
   p.add = add;
   p.scale_log2e = std::max(c->scale * 1.4426950408889634f, 0x1p-100f);  // (the log-sum-exps are divided by it, and it multiplies -inf where a key is not seen)
   p.by_group = fast_div(p.group);
-  const hipError_t e = launch_weigh(p, f.head_dim, f.dtype == KVFOLD_BF16, static_cast<hipStream_t>(stream));
+  const hipError_t e = launch_weigh(p, f.head_dim, f.dtype == KVFOLD_BF16, c->pc.n_cu, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? KVFOLD_OK : hip_fail(e);
 }
 

@@ -10,6 +10,10 @@ namespace kvfold {
 constexpr int kEvictRows = 64;     // rows that a workgroup moves
 constexpr int kEvictPiece = 8192;  // rows that a workgroup looks through where a KV head has several
 
+// Whether wavefronts that weigh the same keys share out the rows, units of 32 of them: where workgroups of 128 keys, wgs of them, leave CUs without
+// work (measured: weigh.hip, launch_width()).
+inline bool weigh_shares_rows(bool bf16, int n_cu, int64_t wgs, int units) { return bf16 ? 2 * wgs < 3 * (int64_t)n_cu && units >= 8 : wgs < n_cu && units >= 4; }
+
 // The caller's workspace of an eviction, in words: kept rows' indices and weights [Hkv][n_keep], per chunk of kEvictRows rows the number of kept
 // rows in front of it [Hkv][chunks + 1] and whether its rows have been read [Hkv][chunks], the next chunk to move; for pieces of long
 // caches the counts of a digit's values [2][Hkv][pieces][256], the rows known to be kept [Hkv][pieces], and what is known of the smallest kept
@@ -64,7 +68,7 @@ struct WeighParams {
   float scale_log2e;
   FastDiv by_group;
 };
-hipError_t launch_weigh(const WeighParams& p, int head_dim, bool bf16, hipStream_t s);
+hipError_t launch_weigh(const WeighParams& p, int head_dim, bool bf16, int n_cu, hipStream_t s);
 
 struct EvictParams {
   const float* weights;     // [Hkv][from_capacity]

@@ -308,36 +308,36 @@ static void launch_f32(const WeighParams& p, hipStream_t s) {
 }
 
 // How a workgroup's wavefronts are shared out between keys and rows.  Neighbouring keys share what is read of the queries; rows are shared out
-// where there are too few keys to fill the chip with workgroups of 128.  bf16, 128 keys a workgroup / 64 keys and four shares of the rows: 256 tokens on 4096 keys,
+// where there are too few keys to fill the chip, of 256 CUs where this was measured, with workgroups of 128.  bf16, 128 keys a workgroup / 64 keys and four shares of the rows: 256 tokens on 4096 keys,
 // 32 heads on 8 (256 workgroups of 128 keys) 21.9 / 17.7 us, 1024 on 1024 84.2 / 39.2, 64 wide 128 on 512, 4 on 1, 11.1 / 6.0; 256 on 32K 92.9 / 115, 32 on
 // 8192 (four units of rows) 7.5 / 11.5.  fp32, 128 keys and two shares / 32 keys and eight: 128 on 4096, 28 on 4, 75.6 / 50.7, 128 on 512, 64 wide, 24.6 / 9.4; 512 on
 // 16K, 8 on 2 (256 workgroups) 159 / 188; one unit of rows has nothing to share out.
 template <int D>
-static void launch_width(const WeighParams& p, bool bf16, hipStream_t s) {
+static void launch_width(const WeighParams& p, bool bf16, int n_cu, hipStream_t s) {
   const int64_t wgs = (int64_t)p.n_kv_heads * ((p.len + 127) / 128);
   const int units = (int)(((int64_t)p.n_tokens * p.group + 31) / 32);
   if (!bf16) {
     if (units == 1)
       launch_f32<D, 8, 1>(p, s);
-    else if (wgs < 256 && units >= 4)
+    else if (weigh_shares_rows(bf16, n_cu, wgs, units))
       launch_f32<D, 1, 8>(p, s);
     else
       launch_f32<D, 4, 2>(p, s);
   } else if (p.n_tokens * p.group <= 16) {
     const dim3 grid((unsigned)((p.len + 255) / 256), (unsigned)p.n_kv_heads);
     hipLaunchKernelGGL(weigh_few_bf16_kernel<D>, grid, dim3(256), 0, s, p);
-  } else if (wgs < 384 && units >= 8) {
+  } else if (weigh_shares_rows(bf16, n_cu, wgs, units)) {
     launch_many<D, 2, 4, 1>(p, s);
   } else {
     launch_many<D, 4, 1, 2>(p, s);
   }
 }
 
-hipError_t launch_weigh(const WeighParams& p, int head_dim, bool bf16, hipStream_t s) {
+hipError_t launch_weigh(const WeighParams& p, int head_dim, bool bf16, int n_cu, hipStream_t s) {
   if (head_dim == 128)
-    launch_width<128>(p, bf16, s);
+    launch_width<128>(p, bf16, n_cu, s);
   else
-    launch_width<64>(p, bf16, s);
+    launch_width<64>(p, bf16, n_cu, s);
   return hipGetLastError();
 }
 

@@ -1,5 +1,5 @@
-// Host model of two rules that the kernels take from the headers that this file includes: who writes the 8-bit cache's ring of bf16 rows, and whom a
-// chunk of an eviction in place waits for.  Workgroups run in any order that the rules allow.
+// Host model of rules that the kernels and their launches take from the headers that this file includes: who writes the 8-bit cache's ring of bf16 rows,
+// whom a chunk of an eviction in place waits for (workgroups run in any order that the rules allow), and how weighing wavefronts are shared out.
 #include <algorithm>
 #include <cstdio>
 #include <cstdlib>
@@ -131,13 +131,23 @@ static void move(std::mt19937& rng, int len, int keep) {
   for (int i = 0; i < keep; ++i) CHECK(cache[(size_t)i] == kept[(size_t)i]);
 }
 
+// The same share of a chip, whatever its CUs are.
+static void weighing() {
+  for (int n_cu : {32, 64, 256, 304})
+    for (int64_t wgs = 1; wgs < 1000; ++wgs) {
+      CHECK(weigh_shares_rows(true, n_cu, wgs, 8) == ((double)wgs < 1.5 * n_cu) && weigh_shares_rows(false, n_cu, wgs, 4) == (wgs < n_cu));
+      CHECK(!weigh_shares_rows(true, n_cu, wgs, 7) && !weigh_shares_rows(false, n_cu, wgs, 3));
+    }
+}
+
 int main() {
   ring();
+  weighing();
   rewound_to_codes();
   std::mt19937 rng(2);
   for (int round = 0; round < 3000; ++round) {
     const int len = 1 + (int)(rng() % 1500);
     move(rng, len, 1 + (int)(rng() % (unsigned)len));
   }
-  std::printf("ok: ring, rewinding, moving in place\n");
+  std::printf("ok: ring, rewinding, weighing, moving in place\n");
 }
