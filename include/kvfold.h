@@ -434,6 +434,105 @@ size_t kvfold_evict_workspace_bytes(const kvfold_cache_t* cache, int64_t n_keep)
 int kvfold_cache_evict(kvfold_cache_t* cache, int layer, const float* weights, int64_t n_keep, int64_t n_sink, int64_t n_recent, kvfold_cache_t* to,
                        int to_layer, float* to_weights, int32_t* kept, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * ---- Many sequences, on a cache in pages -------------------------------------------------------------------------------
+ * The same fold for a batch of sequences that share memory.  A page holds page_tokens rows of K and of V of one layer and every KV head; a sequence's rows
+ * are found by its row of a table, entry p of which is the number of the page with its rows [p page_tokens, (p + 1) page_tokens).  Row r of page n has the
+ * place n * page_tokens + r.  Pages are the same in every layer.  The library keeps no lengths and no tables: they are the caller's, on the device,
+ * so that a captured graph runs on whatever they hold when it is replayed.
+ *
+ * Errors as for kvfold_cache_t: what can be told from the arguments is found before anything is enqueued.  What the device's tables, lengths and
+ * places hold is not looked at by the host and leads nowhere outside the arguments' memory: a table's entry outside [0, n_pages) names no rows (its keys are
+ * seen by nobody), a row whose place is outside the cache is not stored, lengths and counts outside their bounds are taken as the nearest bound.
+ * Nothing allocates or synchronises but create and destroy.  Calls may come from any thread; those that overlap in time have workspaces of their own,
+ * and none reads rows that another stores.
+ */
+typedef struct kvfold_pcache kvfold_pcache_t;
+
+typedef struct {
+  uint32_t struct_size;   /* must be sizeof(kvfold_pcache_config_t)                        */
+  int32_t n_layers, n_q_heads, n_kv_heads, head_dim; /* as kvfold_config_t                 */
+  int32_t page_tokens;    /* 16, 32, 64, 128 or 256                                        */
+  int32_t n_pages;        /* >= 1; n_pages * page_tokens < 2^31                            */
+  int32_t dtype;          /* kvfold_dtype_t                                                */
+  float softmax_scale;    /* 0 selects 1/sqrt(head_dim)                                    */
+  int32_t device;
+  void* kv_buffer;        /* device; optional storage of kvfold_pcache_bytes_required() bytes, 256-byte aligned */
+  size_t kv_buffer_bytes;
+} kvfold_pcache_config_t;
+
+/* Bytes of storage: n_layers * 2 * n_pages * n_kv_heads * page_tokens * head_dim * elem_size.  Host-only; 0 for an invalid configuration. */
+size_t kvfold_pcache_bytes_required(const kvfold_pcache_config_t* cfg /* host */);
+/* Layout: [layer][K, V][page][kv_head][page_tokens][head_dim]. */
+int kvfold_pcache_create(const kvfold_pcache_config_t* cfg, kvfold_pcache_t** out_cache);
+int kvfold_pcache_destroy(kvfold_pcache_t* cache);
+/* Device pointers to the first K and V row of page 0 of `layer`.  Host-only. */
+int kvfold_pcache_view(const kvfold_pcache_t* cache, int layer, void** k_dev, void** v_dev);
+
+/*
+ * Where the new tokens of a batch of requests go, from the requests' lengths, on the device.  Request s holds lens[s] tokens, on ceil(lens[s] / page_tokens)
+ * pages named by its row of the tables, and gets n_new[s] more.  The pages that it lacks come from the end of the free list, in the order of the
+ * requests: with `first` the pages that requests before it lack, its j-th is free_pages[n_free - 1 - first - j].
+ *   lens, n_new   device, [n_seqs]
+ *   free_pages    device, [n_pages]: the first *n_free entries are the numbers of free pages
+ *   n_free        device, [1]; at most n_pages of them count
+ *   tables        device, [n_seqs][table_stride]: the entries of the pages taken are written, no others
+ *   lens_after    device, [n_seqs]: lens + n_new
+ *   cu_new        device, [n_seqs + 1]: the running sum of n_new, from 0
+ *   slots         device, [n_slots]: the place of every new token, packed one request behind the other; -1 behind the last
+ *   positions     device or NULL, [n_slots]: its position in its sequence (for the rotary angles); -1 behind the last
+ *   n_free_after  device, [1]: the free pages left, at the front of the list
+ *   status        device, [1]: 0, or the sum of 1 (more pages lacking than free), 2 (a row of the tables too short), 4 (more new tokens than n_slots) and 8 (a
+ *                 length or count below zero).  Then nothing is assigned: the tables stay, no request has new tokens (cu_new 0, slots -1), lens_after = lens.
+ * All results lie apart from the inputs and from one another, else KVFOLD_ERR_INVALID_ARG (a loop copies lens_after and n_free_after back).
+ * 0 <= n_seqs <= 2^20, 0 <= n_slots < 2^31, 1 <= table_stride < 2^31.  Nothing is allocated; replays of a captured call are as good as the call.
+ */
+int kvfold_pcache_assign(const kvfold_pcache_t* cache, int32_t n_seqs, const int32_t* lens, const int32_t* n_new, const int32_t* free_pages, const int32_t* n_free,
+                         int32_t* tables, int64_t table_stride, int32_t* lens_after, int32_t* cu_new, int64_t* slots, int32_t* positions, int64_t n_slots,
+                         int32_t* n_free_after, int32_t* status, void* stream);
+
+/* A batch: sequence s has the new tokens cu_new[s] .. cu_new[s + 1] - 1 of the packed rows, the last of its lens[s] tokens. */
+typedef struct {
+  uint32_t struct_size;  /* must be sizeof(kvfold_batch_t)                                                                      */
+  int32_t n_seqs;        /* >= 0                                                                                                */
+  int32_t n_tokens;      /* packed rows of q, k_new, v_new, out; those behind cu_new[n_seqs] are left alone                     */
+  int32_t max_new;       /* at least the new tokens of every sequence (tokens beyond are left alone)                            */
+  int64_t max_len;       /* at least every lens[s]; <= 2^30                                                                     */
+  const int32_t* tables; /* device, [n_seqs][table_stride]                                                                      */
+  int64_t table_stride;
+  const int32_t* lens;   /* device, [n_seqs]: tokens of each sequence, the new ones among them                                  */
+  const int32_t* cu_new; /* device, [n_seqs + 1]; or NULL: token s is the only new one of sequence s (n_tokens = n_seqs)        */
+  const int64_t* slots;  /* device, [n_tokens]: places of the new rows, those of the tables; or NULL, with k_new and v_new: they */
+                         /* are there already (kvfold_pcache_append)                                                            */
+  int64_t q_stride;      /* elements from a token's q to the next one's, a multiple of 8 (f32: 4); 0: n_q_heads * head_dim        */
+  int64_t kv_stride;     /* the same of k_new and v_new; 0: n_kv_heads * head_dim                                               */
+} kvfold_batch_t;
+
+/*
+ * Bytes of device memory that kvfold_pcache_step needs for a batch of these numbers (pointers are not looked at).  They have to be zero before the
+ * first use, and every call leaves them so that others with the same n_seqs can follow.  Host-only; 0 for an invalid batch.
+ */
+size_t kvfold_pcache_workspace_bytes(const kvfold_pcache_t* cache, const kvfold_batch_t* batch /* host */);
+
+/*
+ * One fold step of every sequence of the batch on one layer: the new rows are stored at their places, then the i-th of a sequence's n new query rows attends to
+ * the rows j <= lens[s] - n + i that its row of the tables names.  Whole prompts (lens[s] = n), chunks of them and single tokens are the same call; where no
+ * sequence has more than 16 (token, query head) rows a KV head, each sequence's keys are shared out over the GPU.  A sequence with one token beside others with long
+ * prompts is better off in a call of its own.
+ *   q      device, [n_tokens][Hq][d] at q_stride    k_new, v_new  device, [n_tokens][Hkv][d] at kv_stride; 16-byte aligned
+ *   out    device, [n_tokens][Hq][d], 16-byte aligned    lse  device or NULL, [Hq][n_tokens] float, as for kvfold_step_ex
+ *          A row that sees no key, or whose logits are all -inf, gets zeros and -inf.
+ *   workspace  device, 256-byte aligned, at least kvfold_pcache_workspace_bytes() bytes, else KVFOLD_ERR_OOM
+ * A row that the call stores may be seen by one sequence of the batch.  out, lse and the workspace lie apart from all else, and nothing in the cache's
+ * storage, else KVFOLD_ERR_INVALID_ARG.  The same call gives the same bits.
+ */
+int kvfold_pcache_step(const kvfold_pcache_t* cache, int layer, const kvfold_batch_t* batch /* host */, const void* q, const void* k_new, const void* v_new,
+                       void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Rows to their places without attention: k, v and slots as for the step, kv_stride 0 for dense rows. */
+int kvfold_pcache_append(const kvfold_pcache_t* cache, int layer, const void* k, const void* v, int64_t kv_stride, const int64_t* slots, int32_t n_tokens,
+                         void* stream);
+
 /* Static, human-readable name of a status code. */
 const char* kvfold_status_string(int status);
 

@@ -10,5 +10,6 @@ from .binding import (  # noqa: F401
     kvfold_cache_set_length, kvfold_cache_set_storage_roundtrip, kvfold_cache_set_tuning, kvfold_cache_truncate, kvfold_cache_view, kvfold_config_t, kvfold_last_hip_error,
     kvfold_status_string, kvfold_step, kvfold_step_ex, kvfold_step_rope, kvfold_step_window, kvfold_step_noalloc, kvfold_plan_t, kvfold_measure_peaks,
     kvfold_cache_weigh, kvfold_cache_evict, kvfold_evict_workspace_bytes, KvFoldQuantCache, kvfold_qcache_append, kvfold_qcache_bytes_required, kvfold_qcache_create, kvfold_qcache_destroy, kvfold_qcache_length, kvfold_qcache_read,
-    kvfold_qcache_step, kvfold_qcache_truncate,
+    kvfold_qcache_step, kvfold_qcache_truncate, KvFoldBatch, KvFoldPagedCache, kvfold_batch_t, kvfold_pcache_config_t, kvfold_pcache_append, kvfold_pcache_assign,
+    kvfold_pcache_bytes_required, kvfold_pcache_create, kvfold_pcache_destroy, kvfold_pcache_step, kvfold_pcache_view, kvfold_pcache_workspace_bytes,
 )

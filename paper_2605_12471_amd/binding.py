@@ -41,6 +41,18 @@ class kvfold_config_t(ctypes.Structure):
     ]
 
 
+class kvfold_pcache_config_t(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32)] + [(n, ctypes.c_int32) for n in (
+        "n_layers", "n_q_heads", "n_kv_heads", "head_dim", "page_tokens", "n_pages", "dtype")] + [
+        ("softmax_scale", ctypes.c_float), ("device", ctypes.c_int32), ("kv_buffer", ctypes.c_void_p), ("kv_buffer_bytes", ctypes.c_size_t)]
+
+
+class kvfold_batch_t(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("n_seqs", ctypes.c_int32), ("n_tokens", ctypes.c_int32), ("max_new", ctypes.c_int32),
+                ("max_len", ctypes.c_int64), ("tables", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("lens", ctypes.c_void_p),
+                ("cu_new", ctypes.c_void_p), ("slots", ctypes.c_void_p), ("q_stride", ctypes.c_int64), ("kv_stride", ctypes.c_int64)]
+
+
 class kvfold_plan_t(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("n_workgroups", "n_splits", "units_per_wave", "tiles_per_split",
                                               "fused_append", "pair_units", "pair_order")]
@@ -132,6 +144,23 @@ def load_library() -> ctypes.CDLL:
     lib.kvfold_evict_workspace_bytes.restype = ctypes.c_size_t
     lib.kvfold_cache_evict.argtypes = [vp, ctypes.c_int, vp, i64, i64, i64, vp, ctypes.c_int, vp, vp, vp, ctypes.c_size_t, vp]
     lib.kvfold_cache_evict.restype = ctypes.c_int
+    pcfgp, batchp = ctypes.POINTER(kvfold_pcache_config_t), ctypes.POINTER(kvfold_batch_t)
+    lib.kvfold_pcache_bytes_required.argtypes = [pcfgp]
+    lib.kvfold_pcache_bytes_required.restype = ctypes.c_size_t
+    lib.kvfold_pcache_create.argtypes = [pcfgp, ctypes.POINTER(vp)]
+    lib.kvfold_pcache_create.restype = ctypes.c_int
+    lib.kvfold_pcache_destroy.argtypes = [vp]
+    lib.kvfold_pcache_destroy.restype = ctypes.c_int
+    lib.kvfold_pcache_view.argtypes = [vp, ctypes.c_int, ctypes.POINTER(vp), ctypes.POINTER(vp)]
+    lib.kvfold_pcache_view.restype = ctypes.c_int
+    lib.kvfold_pcache_assign.argtypes = [vp, i32, vp, vp, vp, vp, vp, i64, vp, vp, vp, vp, i64, vp, vp, vp]
+    lib.kvfold_pcache_assign.restype = ctypes.c_int
+    lib.kvfold_pcache_workspace_bytes.argtypes = [vp, batchp]
+    lib.kvfold_pcache_workspace_bytes.restype = ctypes.c_size_t
+    lib.kvfold_pcache_step.argtypes = [vp, ctypes.c_int, batchp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.kvfold_pcache_step.restype = ctypes.c_int
+    lib.kvfold_pcache_append.argtypes = [vp, ctypes.c_int, vp, vp, i64, vp, i32, vp]
+    lib.kvfold_pcache_append.restype = ctypes.c_int
     lib.kvfold_last_hip_error.argtypes = []
     lib.kvfold_last_hip_error.restype = ctypes.c_int
     _lib = lib
@@ -288,6 +317,52 @@ def kvfold_qcache_length(cache, layer) -> int:
 
 def kvfold_qcache_truncate(cache, layer, new_len) -> int:
     return load_library().kvfold_qcache_truncate(cache, layer, new_len)
+
+
+def make_pconfig(n_layers, n_q_heads, n_kv_heads, head_dim, page_tokens, n_pages, dtype, softmax_scale=0.0, device=0, kv_buffer=None, kv_buffer_bytes=0):
+    return kvfold_pcache_config_t(ctypes.sizeof(kvfold_pcache_config_t), n_layers, n_q_heads, n_kv_heads, head_dim, page_tokens, n_pages, dtype, softmax_scale,
+                                  device, kv_buffer, kv_buffer_bytes)
+
+
+def make_batch(n_seqs, n_tokens, max_new, max_len, tables=None, table_stride=1, lens=None, cu_new=None, slots=None, q_stride=0, kv_stride=0):
+    return kvfold_batch_t(ctypes.sizeof(kvfold_batch_t), n_seqs, n_tokens, max_new, max_len, tables, table_stride, lens, cu_new, slots, q_stride, kv_stride)
+
+
+def kvfold_pcache_bytes_required(cfg) -> int:
+    return int(load_library().kvfold_pcache_bytes_required(ctypes.byref(cfg)))
+
+
+def kvfold_pcache_create(cfg):
+    h = ctypes.c_void_p()
+    rc = load_library().kvfold_pcache_create(ctypes.byref(cfg) if cfg is not None else None, ctypes.byref(h))
+    return rc, (h if rc == 0 else None)
+
+
+def kvfold_pcache_destroy(cache) -> int:
+    return load_library().kvfold_pcache_destroy(cache)
+
+
+def kvfold_pcache_view(cache, layer):
+    k, v = ctypes.c_void_p(), ctypes.c_void_p()
+    return load_library().kvfold_pcache_view(cache, layer, ctypes.byref(k), ctypes.byref(v)), k.value, v.value
+
+
+def kvfold_pcache_assign(cache, n_seqs, lens, n_new, free_pages, n_free, tables, table_stride, lens_after, cu_new, slots, positions, n_slots, n_free_after, status,
+                         stream=0) -> int:
+    return load_library().kvfold_pcache_assign(cache, n_seqs, lens, n_new, free_pages, n_free, tables, table_stride, lens_after, cu_new, slots, positions, n_slots,
+                                               n_free_after, status, stream)
+
+
+def kvfold_pcache_workspace_bytes(cache, batch) -> int:
+    return int(load_library().kvfold_pcache_workspace_bytes(cache, ctypes.byref(batch) if batch is not None else None))
+
+
+def kvfold_pcache_step(cache, layer, batch, q, k_new, v_new, out, lse, workspace, workspace_bytes, stream=0) -> int:
+    return load_library().kvfold_pcache_step(cache, layer, ctypes.byref(batch) if batch is not None else None, q, k_new, v_new, out, lse, workspace, workspace_bytes, stream)
+
+
+def kvfold_pcache_append(cache, layer, k, v, kv_stride, slots, n_tokens, stream=0) -> int:
+    return load_library().kvfold_pcache_append(cache, layer, k, v, kv_stride, slots, n_tokens, stream)
 
 
 def kvfold_status_string(status: int) -> str:
@@ -776,3 +851,153 @@ class KvFoldQuantCache:
         rc = self._lib.kvfold_qcache_truncate(self.handle, layer, new_len)
         if rc:
             raise KvFoldError(rc, "kvfold_qcache_truncate")
+
+
+class KvFoldPagedCache:
+    """Owns one cache in pages (``kvfold_pcache_*``), which sequences share; tables, lengths and places are tensors of the caller's, in a ``KvFoldBatch``."""
+
+    def __init__(self, n_layers, n_q_heads, n_kv_heads, head_dim, page_tokens, n_pages, dtype="bf16", softmax_scale=0.0, device=0):
+        import torch
+        self.dtype_name = dtype
+        self.cfg = make_pconfig(n_layers, n_q_heads, n_kv_heads, head_dim, page_tokens, n_pages, {"f32": KVFOLD_F32, "bf16": KVFOLD_BF16}[dtype], softmax_scale,
+                                device)
+        self.handle = None
+        rc, self.handle = kvfold_pcache_create(self.cfg)
+        if rc:
+            raise KvFoldError(rc, "kvfold_pcache_create")
+        self._dtype, self._f32, self._i32, self._i64 = torch.float32 if dtype == "f32" else torch.bfloat16, torch.float32, torch.int32, torch.int64
+        self._device, self._hq, self._hkv, self._d, self._page, self._n_pages, self._n_layers = device, n_q_heads, n_kv_heads, head_dim, page_tokens, n_pages, n_layers
+        self._lib = load_library()
+
+    def close(self):
+        if getattr(self, "handle", None) is not None:
+            rc = kvfold_pcache_destroy(self.handle)
+            self.handle = None
+            if rc:
+                raise KvFoldError(rc, "kvfold_pcache_destroy")
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def _stream(self, stream):
+        return _current_stream(self._device) if stream is None else stream
+
+    def _rows(self, name, t, n, heads):
+        """Address and token stride of [n][heads][d] rows whose heads lie side by side, as parts of a fused projection's result do."""
+        _expect(name, t, self._dtype, self._device, (n, heads, self._d), contiguous=False)
+        if n and ((heads > 1 and t.stride(1) != self._d) or t.stride(2) != 1 or (n > 1 and t.stride(0) < heads * self._d)):
+            raise ValueError(f"{name}: expected a token's heads side by side, got strides {t.stride()}")
+        return t.data_ptr(), t.stride(0) if n > 1 else heads * self._d
+
+    def assign(self, batch, lens, n_new, free_pages, n_free, stream=None):
+        """Where the new tokens of the batch's sequences go, into the batch's own tensors (tables, lens, cu_new, slots, positions, n_free, status): lens, n_new int32
+        [n_seqs], free_pages int32 [n_pages], n_free int32 [1].  Nothing is synchronised: status says on the device whether there was room."""
+        s = batch.n_seqs
+        rc = self._lib.kvfold_pcache_assign(
+            self.handle, s, _expect("lens", lens, self._i32, self._device, (s,)), _expect("n_new", n_new, self._i32, self._device, (s,)),
+            _expect("free_pages", free_pages, self._i32, self._device, (self._n_pages,)), _expect("n_free", n_free, self._i32, self._device, (1,)),
+            batch.tables.data_ptr(), batch.tables.shape[1], batch.lens.data_ptr(), batch.cu_new.data_ptr(), batch.slots.data_ptr(), batch.positions.data_ptr(),
+            batch.n_tokens, batch.n_free.data_ptr(), batch.status.data_ptr(), self._stream(stream))
+        if rc:
+            raise KvFoldError(rc, "kvfold_pcache_assign")
+        return batch
+
+    def step(self, layer, batch, q, k_new, v_new, out, lse=None, stream=None):
+        """Enqueue one fold step of every sequence of the batch: q, out [n_tokens][Hq][d], k_new, v_new [n_tokens][Hkv][d], lse fp32 [Hq][n_tokens].  q, k_new and v_new
+        may be parts of one tensor.  k_new = v_new = None: the new rows are in the pages already (``append``)."""
+        n = batch.n_tokens
+        desc = batch.desc
+        q_at, q_stride = self._rows("q", q, n, self._hq)
+        k_at = v_at = None
+        kv_stride, slots = 0, None
+        if (k_new is None) != (v_new is None):
+            raise ValueError("k_new and v_new: both or neither")
+        if k_new is not None:
+            (k_at, kv_stride), (v_at, v_stride) = self._rows("k_new", k_new, n, self._hkv), self._rows("v_new", v_new, n, self._hkv)
+            if v_stride != kv_stride:
+                raise ValueError(f"v_new: expected the strides of k_new, got {v_new.stride()} beside {k_new.stride()}")
+            slots = batch.slots.data_ptr()
+        step_batch = kvfold_batch_t.from_buffer_copy(desc)
+        step_batch.q_stride, step_batch.kv_stride, step_batch.slots = q_stride, kv_stride, slots
+        rc = self._lib.kvfold_pcache_step(
+            self.handle, layer, ctypes.byref(step_batch), q_at, k_at, v_at, _expect("out", out, self._dtype, self._device, (n, self._hq, self._d)),
+            None if lse is None else _expect("lse", lse, self._f32, self._device, (self._hq, n)), batch.workspace.data_ptr(), batch.workspace.numel(), self._stream(stream))
+        if rc:
+            raise KvFoldError(rc, "kvfold_pcache_step")
+        return out
+
+    def append(self, layer, k, v, slots, stream=None):
+        """Rows k, v [n][Hkv][d] to their places, slots int64 [n], without attention; a place outside the cache (-1) is passed over."""
+        n = k.shape[0] if k.dim() == 3 else -1
+        (k_at, stride), (v_at, v_stride) = self._rows("k", k, n, self._hkv), self._rows("v", v, n, self._hkv)
+        if v_stride != stride:
+            raise ValueError(f"v: expected the strides of k, got {v.stride()} beside {k.stride()}")
+        rc = self._lib.kvfold_pcache_append(self.handle, layer, k_at, v_at, stride, _expect("slots", slots, self._i64, self._device, (n,)), n, self._stream(stream))
+        if rc:
+            raise KvFoldError(rc, "kvfold_pcache_append")
+
+    def bytes_required(self) -> int:
+        return kvfold_pcache_bytes_required(self.cfg)
+
+    def view(self, layer=0):
+        """Torch tensors aliasing the layer's K and V pages, [n_pages][Hkv][page_tokens][d] each; they keep the cache."""
+        import torch
+        rc, k, v = kvfold_pcache_view(self.handle, layer)
+        if rc:
+            raise KvFoldError(rc, "kvfold_pcache_view")
+        shape = (self._n_pages, self._hkv, self._page, self._d)
+        return tuple(_alias(self, at, shape, self._dtype, f"cuda:{self._device}", torch) for at in (k, v))
+
+
+def _alias(owner, at, shape, dtype, device, torch):
+    class Memory:  # (no bf16 in this protocol: 16-bit whole numbers, then viewed)
+        __cuda_array_interface__ = {"shape": shape, "typestr": "<i2" if dtype == torch.bfloat16 else "<f4", "data": (at, False), "version": 3, "strides": None}
+    memory = Memory()
+    memory.owner = owner
+    t = torch.as_tensor(memory, device=device)
+    return t.view(dtype) if t.dtype != dtype else t
+
+
+class KvFoldBatch:
+    """A batch of sequences for ``KvFoldPagedCache``: the tables [n_seqs][pages] int32, which are the caller's, and what goes with them, made here where not
+    given: lens int32 [n_seqs] (the new tokens among them), cu_new int32 [n_seqs + 1], slots int64 [n_tokens], and the workspace of its steps.
+
+    n_tokens rows are packed in a step's tensors; max_new and max_len bound the new tokens and the tokens of any sequence.  one_each: every sequence has
+    exactly one new token, and n_tokens = n_seqs.  A batch is good for one step at a time: steps that may overlap (on streams of their own) have a batch each.
+    What is made here is made on the current stream: a step on another one waits for it."""
+
+    def __init__(self, cache, tables, n_tokens, max_new, max_len, lens=None, cu_new=None, slots=None, one_each=False):
+        import torch
+        dev = cache._device
+        _expect("tables", tables, torch.int32, dev)
+        if tables.dim() != 2 or not tables.shape[1]:
+            raise ValueError(f"tables: expected [n_seqs][pages], got {tuple(tables.shape)}")
+        self.cache, self.tables, self.n_seqs, self.n_tokens, self.one_each = cache, tables, tables.shape[0], n_tokens, one_each
+        where = f"cuda:{dev}"
+
+        def mine(name, given, shape, dtype):
+            if given is None:
+                return torch.zeros(shape, dtype=dtype, device=where)
+            _expect(name, given, dtype, dev, shape)
+            return given
+        if n_tokens < 0:
+            raise ValueError(f"n_tokens: expected at least 0, got {n_tokens}")
+        self.lens = mine("lens", lens, (self.n_seqs,), torch.int32)
+        self.cu_new = mine("cu_new", cu_new, (self.n_seqs + 1,), torch.int32)
+        self.slots = mine("slots", slots, (n_tokens,), torch.int64)
+        self.positions, self.n_free, self.status = (torch.zeros(shape, dtype=torch.int32, device=where) for shape in ((n_tokens,), (1,), (1,)))
+        self.desc = make_batch(self.n_seqs, n_tokens, max_new, max_len, tables.data_ptr(), tables.shape[1], self.lens.data_ptr(),
+                               None if one_each else self.cu_new.data_ptr(), None)
+        need = kvfold_pcache_workspace_bytes(cache.handle, self.desc)
+        if not need:
+            raise ValueError(f"a batch of {self.n_seqs} sequences, {n_tokens} tokens, max_new {max_new}, max_len {max_len} is none")
+        self.workspace = torch.zeros((need,), dtype=torch.uint8, device=where)

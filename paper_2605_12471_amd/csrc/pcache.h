@@ -1,0 +1,115 @@
+// The cache in pages: what its kernels, its planner and the host model of both share.
+#pragma once
+#include <stddef.h>
+#include <stdint.h>
+
+#include "kvfold_consts.h"
+#include "kvfold_plan.h"
+
+namespace kvfold {
+
+constexpr int64_t kPagedMaxRows = 1 << 20;  // (row, piece) pairs of a workspace
+constexpr int kPagedMeetStride = 16;        // words from one unit's counter to the next: a line's
+constexpr int kPagedMaxPieces = 128;        // of a sequence's keys
+
+int validate_pconfig(const kvfold_pcache_config_t* c);
+size_t pcache_layer_bytes(const kvfold_pcache_config_t& c);  // K and V
+// What can be told from a batch's numbers, without its pointers
+int validate_batch(const kvfold_pcache_config_t& c, const kvfold_batch_t* b);
+
+struct PagedPlan {
+  bool decode;           // at most 16 packed rows per sequence and KV head: the kernel that deals keys to wavefronts
+  int unit_rows;         // packed rows of a workgroup (decode: of a sequence and KV head)
+  int units_per_wave;    // prompts: 32-row units of a wavefront
+  int64_t blocks;        // prompts: workgroups per KV head and piece, an upper bound of those with rows
+  int n_pieces;          // of the keys, at most
+  int piece;             // keys of one, a multiple of 128
+  int64_t rows;          // of partial results
+  size_t counters;       // bytes in front of them, of the counters by which pieces meet
+  size_t bytes;          // of the workspace
+};
+PagedPlan make_pplan(const kvfold_pcache_config_t& c, int n_cu, const kvfold_batch_t& b);
+
+// Prompts: the workgroups of sequence s, whose new tokens are first .. first + n - 1 of the packed ones, are numbered from here on; each has unit_rows packed rows
+// of the sequence.  (For any first tokens that ascend: floor(a + x) - floor(a) + 1 >= ceil(x), so that the numbers of two sequences never meet.)
+KVFOLD_HD int64_t paged_first_block(int64_t first, int s, int G, int unit_rows) { return first * G / unit_rows + s; }
+
+// The pieces of `len` keys, one at least
+KVFOLD_HD int paged_pieces(int len, int piece) {
+  const int n = (int)(((unsigned)len + (unsigned)piece - 1) / (unsigned)piece);
+  return n < 1 ? 1 : n;
+}
+
+// A sequence's new tokens and its length from what the device holds, inside the batch's bounds whatever that is: tokens [first, first + n) exist, n <= max_new,
+// 0 <= len <= max_len.
+struct PagedSeq {
+  int first, n, len;
+};
+KVFOLD_HD PagedSeq paged_seq(int from, int to, int len, int n_tokens, int max_new, int max_len) {
+  PagedSeq q;
+  q.first = from < 0 ? 0 : from > n_tokens ? n_tokens : from;
+  const int end = to < q.first ? q.first : to > n_tokens ? n_tokens : to;
+  q.n = end - q.first < max_new ? end - q.first : max_new;
+  q.len = len < 0 ? 0 : len > max_len ? max_len : len;
+  return q;
+}
+
+}  // namespace kvfold
+
+#if defined(__HIP__)
+#include <hip/hip_runtime.h>
+
+namespace kvfold {
+
+struct AssignParams {
+  const int32_t *lens, *n_new, *free_pages, *n_free;
+  int32_t *tables, *lens_after, *cu_new, *positions, *n_free_after, *status;
+  int64_t* slots;
+  int64_t table_stride, n_slots;
+  int32_t n_seqs, page_log2, n_pages;
+};
+hipError_t launch_assign(const AssignParams& p, int n_cu, hipStream_t s);
+
+struct PAppendParams {
+  const void *k, *v;  // [n_tokens][Hkv][d] at token_bytes
+  void *k_pages, *v_pages;
+  const int64_t* slots;
+  int64_t token_bytes;
+  int64_t n_places;
+  int32_t n_tokens, n_kv_heads, row_bytes, page_log2;
+};
+hipError_t launch_pappend(const PAppendParams& p, hipStream_t s);
+
+struct PAttnParams {
+  const void* q;
+  const void *k_new, *v_new;  // nullptr: the new rows are in the pages
+  void *k_pages, *v_pages;    // of the layer
+  void* out;
+  float* lse;
+  const int32_t *tables, *lens, *cu_new;
+  const int64_t* slots;
+  uint32_t* counters;  // zero between steps
+  float *part_o, *part_ml;
+  int64_t table_stride, q_stride, kv_stride;  // (the latter two in elements)
+  int64_t n_places;
+  uint64_t page_bytes;  // of K or V of a page
+  int32_t n_seqs, n_tokens, max_new, max_len;  // (max_len: also what a row of the tables can name)
+  int32_t n_q_heads, n_kv_heads, group, page_log2, n_pages;
+  int32_t n_pieces, piece, unit_rows;
+  int32_t n_units;  // decode: sequences times KV heads; prompts: blocks
+  float scale_log2e;
+  FastDiv by_group, by_units, by_kv_heads;
+};
+hipError_t launch_attn_pdecode(const PAttnParams& p, int head_dim, bool bf16, hipStream_t s);
+hipError_t launch_attn_prompt(const PAttnParams& p, int head_dim, bool bf16, int units_per_wave, hipStream_t s);
+hipError_t prepare_attn_prompt(int head_dim, bool bf16);
+hipError_t prepare_attn_prompt_f32(int head_dim);
+hipError_t launch_attn_prompt_f32(const PAttnParams& p, int head_dim, hipStream_t s);
+hipError_t launch_pmerge(const PAttnParams& p, int head_dim, bool bf16, hipStream_t s);
+
+// Read-only arguments by scalar loads (nobody writes them while the kernel runs)
+template <class T>
+using ConstPtr = const __attribute__((address_space(4))) T*;
+
+}  // namespace kvfold
+#endif

@@ -1,0 +1,81 @@
+// Host decisions of the cache in pages.  No HIP in this file.
+#include <algorithm>
+#include <cmath>
+
+#include "pcache.h"
+
+namespace kvfold {
+
+int validate_pconfig(const kvfold_pcache_config_t* c) {
+  if (!c || c->struct_size != sizeof(kvfold_pcache_config_t)) return KVFOLD_ERR_INVALID_ARG;
+  if (c->n_layers < 1 || c->n_q_heads < 1 || c->n_kv_heads < 1 || c->n_pages < 1 || c->page_tokens < 1 || c->device < 0 || !(c->softmax_scale >= 0.f) ||
+      !std::isfinite(c->softmax_scale))
+    return KVFOLD_ERR_INVALID_ARG;
+  if (c->kv_buffer && (reinterpret_cast<uintptr_t>(c->kv_buffer) & 255)) return KVFOLD_ERR_INVALID_ARG;
+  if (elem_size(c->dtype) == 0) return KVFOLD_ERR_UNSUPPORTED;
+  if (c->head_dim != 64 && c->head_dim != 128) return KVFOLD_ERR_UNSUPPORTED;
+  if (c->n_q_heads % c->n_kv_heads || c->n_kv_heads > 32767 || c->n_q_heads > 1 << 20) return KVFOLD_ERR_UNSUPPORTED;
+  if (c->page_tokens < 16 || c->page_tokens > 256 || (c->page_tokens & (c->page_tokens - 1))) return KVFOLD_ERR_UNSUPPORTED;
+  if ((int64_t)c->n_pages * c->page_tokens >= (int64_t)1 << 31) return KVFOLD_ERR_UNSUPPORTED;
+  // (all bytes in 64 bits: n_layers < 2^31 times a page pool's at most 2^31 * 2^15 * 2^9 * 2)
+  if ((double)c->n_layers * (double)pcache_layer_bytes(*c) > 9e18) return KVFOLD_ERR_UNSUPPORTED;
+  return KVFOLD_OK;
+}
+
+size_t pcache_layer_bytes(const kvfold_pcache_config_t& c) {
+  return 2u * (size_t)c.n_pages * (size_t)c.n_kv_heads * (size_t)c.page_tokens * (size_t)c.head_dim * (size_t)elem_size(c.dtype);
+}
+
+int validate_batch(const kvfold_pcache_config_t& c, const kvfold_batch_t* b) {
+  if (!b || b->struct_size != sizeof(kvfold_batch_t)) return KVFOLD_ERR_INVALID_ARG;
+  if (b->n_seqs < 0 || b->n_tokens < 0 || b->max_new < 1 || b->max_len < 1 || b->table_stride < 1 || b->q_stride < 0 || b->kv_stride < 0)
+    return KVFOLD_ERR_INVALID_ARG;
+  const int64_t unit = 16 / elem_size(c.dtype), wide = (int64_t)c.n_q_heads * c.head_dim, narrow = (int64_t)c.n_kv_heads * c.head_dim;
+  if (b->q_stride % unit || b->kv_stride % unit || (b->q_stride && b->q_stride < wide) || (b->kv_stride && b->kv_stride < narrow)) return KVFOLD_ERR_INVALID_ARG;
+  if (b->max_len > (int64_t)1 << 30 || b->table_stride >= (int64_t)1 << 31 || (int64_t)b->n_tokens * c.n_q_heads > (int64_t)1 << 28 || b->n_seqs > 1 << 20 ||
+      (int64_t)b->n_seqs * c.n_kv_heads > (int64_t)1 << 24 || b->q_stride > (int64_t)1 << 31 || b->kv_stride > (int64_t)1 << 31)
+    return KVFOLD_ERR_UNSUPPORTED;
+  return KVFOLD_OK;
+}
+
+PagedPlan make_pplan(const kvfold_pcache_config_t& c, int n_cu, const kvfold_batch_t& b) {
+  const int G = c.n_q_heads / c.n_kv_heads;
+  const int64_t max_new = std::min<int64_t>(b.max_new, std::max(b.n_tokens, 1)), len = std::min(b.max_len, b.table_stride * c.page_tokens);
+  const int64_t steps = (len + 127) / 128;  // (pieces are whole steps of 128 keys)
+  PagedPlan pl{};
+  pl.decode = max_new * G <= 16;
+  int64_t pieces;
+  const int64_t units = std::max<int64_t>(1, (int64_t)b.n_seqs * c.n_kv_heads);
+  if (pl.decode) {
+    pl.unit_rows = (int)max_new * G;
+    pl.units_per_wave = 1;
+    pieces = std::max((2 * n_cu + units - 1) / units, (len + 2047) / 2048);
+    pieces = std::min(pieces, kPagedMaxRows / (units * pl.unit_rows));
+    pieces = std::max<int64_t>(1, std::min<int64_t>({pieces, steps, kPagedMaxPieces}));
+    pl.piece = (int)((steps + pieces - 1) / pieces) * 128;
+    pl.n_pieces = paged_pieces((int)len, pl.piece);
+    pl.rows = pl.n_pieces > 1 ? units * pl.n_pieces * pl.unit_rows : 0;
+  } else {
+    pl.units_per_wave = 1;
+    pl.unit_rows = kUnitsPerWg * kRowsPerUnit * pl.units_per_wave;
+    pl.blocks = (int64_t)b.n_tokens * G / pl.unit_rows + b.n_seqs;
+    const int64_t rows = (int64_t)b.n_tokens * c.n_q_heads, wgs = std::max<int64_t>(1, ((int64_t)b.n_tokens * G + pl.unit_rows - 1) / pl.unit_rows * c.n_kv_heads);
+    pieces = std::max<int64_t>(1, 2 * n_cu / wgs);
+    pieces = std::min(pieces, kPagedMaxRows / std::max<int64_t>(rows, 1));
+    pieces = std::max<int64_t>(1, std::min<int64_t>({pieces, steps, 16}));
+    pl.piece = (int)((steps + pieces - 1) / pieces) * 128;
+    pl.n_pieces = paged_pieces((int)len, pl.piece);
+    pl.rows = pl.n_pieces > 1 ? rows * pl.n_pieces : 0;
+  }
+  pl.counters = ((size_t)units * kPagedMeetStride * sizeof(uint32_t) + 255) / 256 * 256;  // (always there: steps of either kind share a workspace)
+  pl.bytes = pl.counters + (((size_t)pl.rows * (size_t)(c.head_dim + 2) * sizeof(float)) + 255) / 256 * 256;
+  return pl;
+}
+
+}  // namespace kvfold
+
+using namespace kvfold;
+
+extern "C" size_t kvfold_pcache_bytes_required(const kvfold_pcache_config_t* cfg) {
+  return validate_pconfig(cfg) == KVFOLD_OK ? (size_t)cfg->n_layers * pcache_layer_bytes(*cfg) : 0;
+}
