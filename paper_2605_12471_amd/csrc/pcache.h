@@ -97,7 +97,7 @@ struct PAttnParams {
   int32_t n_q_heads, n_kv_heads, group, page_log2, n_pages;
   int32_t n_pieces, piece, unit_rows;
   int32_t n_units;  // decode: sequences times KV heads; prompts: blocks
-  float scale_log2e;
+  float scale_log2e, from_log2, stale;  // its reciprocal, and 2^16 in its units
   FastDiv by_group, by_units, by_kv_heads;
 };
 hipError_t launch_attn_pdecode(const PAttnParams& p, int head_dim, bool bf16, hipStream_t s);

@@ -246,6 +246,8 @@ int kvfold_pcache_step(const kvfold_pcache_t* c, int layer, const kvfold_batch_t
   p.unit_rows = pl.unit_rows;
   p.n_units = pl.decode ? b->n_seqs * f.n_kv_heads : (int32_t)pl.blocks;
   p.scale_log2e = c->scale * 1.4426950408889634f;
+  p.from_log2 = 1.0f / p.scale_log2e;
+  p.stale = 16.0f * p.from_log2;
   p.by_group = fast_div(p.group);
   p.by_units = fast_div(p.n_units);
   p.by_kv_heads = fast_div(f.n_kv_heads);
