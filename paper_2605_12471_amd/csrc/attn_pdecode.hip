@@ -14,8 +14,6 @@
 //
 // bf16: neither queries nor keys are rounded on the way, P = 2^(S scale log2 e - m) is for P V (attn_decode.hip's rounding points but for the query's), row sums are
 // fp32 from the unrounded P, m is stale by at most 2^16.
-#include <type_traits>
-
 #include "meet.h"
 #include "pcache.h"
 
@@ -29,7 +27,7 @@ typedef __attribute__((ext_vector_type(2))) unsigned uintx2;
 typedef __attribute__((ext_vector_type(4))) float floatx4;
 typedef __attribute__((ext_vector_type(2))) float floatx2;
 
-constexpr int kPDecodeWaves = 4;
+constexpr int kPDecodeWaves = 4;  // (eight: never better, 300 keys 9.6 us for 8.8, 64 sequences of 500 31 for 26)
 
 template <class T, int D>
 __global__ void __launch_bounds__(kPDecodeWaves * 64, 2) attn_pdecode_kernel(PAttnParams p) {
@@ -48,8 +46,22 @@ __global__ void __launch_bounds__(kPDecodeWaves * 64, 2) attn_pdecode_kernel(PAt
   __shared__ floatx2 red_ml[NW * ROWS];
   __shared__ int last;
 
-  const int piece = (int)quot(blockIdx.x, p.by_units), unit = (int)blockIdx.x - piece * p.n_units;
+  // (every line of the arguments is fetched now, in one round trip)
+  asm volatile("" ::"s"(p.q), "s"(p.out), "s"(p.slots), "s"(p.table_stride), "s"(p.n_seqs), "s"(p.n_pieces), "s"(p.by_kv_heads.mul));
+  // The longest sequences' last pieces first, which are whole; everybody's first one, which is what is left of its length, at the end.
+  const int n_before = (int)quot(blockIdx.x, p.by_units), unit = (int)blockIdx.x - n_before * p.n_units, piece = p.n_pieces - 1 - n_before;
   const int seq = (int)quot((unsigned)unit, p.by_kv_heads), g = unit - seq * p.n_kv_heads;
+  const int tid = threadIdx.x, l = tid & 63, kg = l >> 4, c16 = l & 15;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int32_t* table = p.tables + (int64_t)seq * p.table_stride;
+  int pages[TILES];  // lane l: of the wavefront's block (the last multiple of 64) + l
+  if (!p.from_end) {  // where a piece begins is known: its pages are asked for together with the lengths (a tenth of the time of a short sequence's step)
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) {
+      const int64_t column = (((int64_t)piece * (p.piece / BK) + w + NW * l) * BK + 16 * t) >> p.page_log2;
+      pages[t] = column < p.table_stride ? table[column] : -1;
+    }
+  }
   PagedSeq sq;
   {
     const int len = ((ConstPtr<int32_t>)(uintptr_t)p.lens)[seq];
@@ -63,14 +75,16 @@ __global__ void __launch_bounds__(kPDecodeWaves * 64, 2) attn_pdecode_kernel(PAt
   const int n_pieces = paged_pieces(sq.len, p.piece);
   if (sq.n == 0 || piece >= n_pieces) return;
 
-  const int tid = threadIdx.x, l = tid & 63, kg = l >> 4, c16 = l & 15;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int Hq = p.n_q_heads, G = p.group, rows = sq.n * G, prev = sq.len - sq.n;
 
   // ---- the wavefront's blocks: every NW-th of the piece's.  New rows lie in the sequence's last two at most, so that a wavefront has at most one with new
   // rows, its last.
-  const int b_begin = piece * (p.piece / BK), b_all = (sq.len + BK - 1) / BK;
-  const int b_end = b_begin + p.piece / BK < b_all ? b_begin + p.piece / BK : b_all;
+  const int b_all = (sq.len + BK - 1) / BK, per_piece = p.piece / BK;
+  int b_begin = piece * per_piece, b_end = b_begin + per_piece < b_all ? b_begin + per_piece : b_all;
+  if (p.from_end) {  // what is left of the length is the first piece's
+    b_end = b_all - (n_pieces - 1 - piece) * per_piece;
+    b_begin = piece == 0 ? 0 : b_end - per_piece;
+  }
   const int b_first = b_begin + w, n_blocks = b_first < b_end ? (int)((unsigned)(b_end - b_first + NW - 1) / (unsigned)NW) : 0;
   const bool fresh = p.k_new != nullptr;
   const int old = !fresh ? sq.len : prev > 0 ? prev : 0;  // rows that are read from the pages
@@ -78,18 +92,17 @@ __global__ void __launch_bounds__(kPDecodeWaves * 64, 2) attn_pdecode_kernel(PAt
   const bool special = n_blocks > 0 && (b_last + 1) * BK > old && fresh;
   const int n_plain = n_blocks - (special ? 1 : 0);
 
-  const int32_t* table = p.tables + (int64_t)seq * p.table_stride;
   const int key_end = b_end * BK < sq.len ? b_end * BK : sq.len;
-  int pages[TILES];  // lane l: of the wavefront's block (the last multiple of 64) + l
-  auto fetch_pages = [&](int i0) __attribute__((always_inline)) {
+  auto fetch_pages = [&](int i0, bool there) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
       const int key = (b_first + NW * (i0 + l)) * BK + 16 * t;
-      pages[t] = -1;
-      if (i0 + l < n_blocks && key < key_end) pages[t] = table[(unsigned)key >> p.page_log2];
+      const bool mine = i0 + l < n_blocks && key < key_end;
+      if (!there && mine) pages[t] = table[(unsigned)key >> p.page_log2];
+      if (!mine) pages[t] = -1;
     }
   };
-  fetch_pages(0);
+  fetch_pages(0, !p.from_end);
 
   // ---- Q: lane (c16, kg) holds the columns of row c16 that its shares of the K rows have
   const int row = c16 < rows ? c16 : rows - 1, tok = (int)quot((unsigned)row, p.by_group);
@@ -101,6 +114,7 @@ __global__ void __launch_bounds__(kPDecodeWaves * 64, 2) attn_pdecode_kernel(PAt
     for (int v = 0; v < KV; ++v) qf[v] = *reinterpret_cast<const uintx4*>(reinterpret_cast<const unsigned char*>(qrow) + v * 64 + kg * 16);
   }
 
+  int limit = sq.len;  // keys from it on are taken as zeros
   struct Block {
     uintx4 k[TILES][KV];
     vvec v[TILES][4][VV];
@@ -109,7 +123,7 @@ __global__ void __launch_bounds__(kPDecodeWaves * 64, 2) attn_pdecode_kernel(PAt
   const unsigned k_lane = (unsigned)c16 * ROWB + (unsigned)kg * 16, v_lane = (unsigned)(4 * kg) * ROWB + (unsigned)c16 * (VWORDS * 4);
   const uint64_t head = (uint64_t)(unsigned)g * ((uint64_t)(unsigned)ROWB << p.page_log2);
   auto load_tile = [&](Block& x, int t, int page, int key0) __attribute__((always_inline)) {
-    int n = old - key0;
+    int n = (old < limit ? old : limit) - key0;
     n = n < 0 ? 0 : n > 16 ? 16 : n;
     const bool there = (unsigned)page < (unsigned)p.n_pages;
     const uint64_t at = (uint64_t)(unsigned)(there ? page : 0) * p.page_bytes + head + (unsigned)((key0 & ((1 << p.page_log2) - 1)) * ROWB);
@@ -131,7 +145,7 @@ __global__ void __launch_bounds__(kPDecodeWaves * 64, 2) attn_pdecode_kernel(PAt
   };
   // Block i of the wavefront's; past the plain ones there is nothing to ask for, and nothing is
   auto load = [&](Block& x, int i) __attribute__((always_inline)) {
-    if ((i & 63) == 0 && i > 0 && i < n_plain) fetch_pages(i);
+    if ((i & 63) == 0 && i > 0 && i < n_plain) fetch_pages(i, false);
     x.gone = 0;
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
@@ -141,17 +155,9 @@ __global__ void __launch_bounds__(kPDecodeWaves * 64, 2) attn_pdecode_kernel(PAt
   };
 
   floatx4 o[J];
-  float m_run = -INFINITY, l_run = 0.f;
-#pragma unroll
-  for (int j = 0; j < J; ++j) o[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  float m_run, l_run;
 
-  // O^T += V^T P^T (into acc), with the keys from `limit` on left out where CUT
-  auto outputs = [&](const Block& x, const floatx4 (&pw)[TILES], auto&& into, int rel_limit, auto cut) __attribute__((always_inline)) {
-    constexpr bool CUT = decltype(cut)::value;
-    auto word = [&](int t, int r, int j, int i) __attribute__((always_inline)) -> unsigned {
-      const unsigned u = x.v[t][r][j][i];
-      return CUT && 16 * t + 4 * kg + r >= rel_limit ? 0u : u;
-    };
+  auto outputs = [&](const Block& x, const floatx4 (&pw)[TILES]) __attribute__((always_inline)) {
     if constexpr (BF16) {
       uintx4 pb;
 #pragma unroll
@@ -168,19 +174,14 @@ __global__ void __launch_bounds__(kPDecodeWaves * 64, 2) attn_pdecode_kernel(PAt
         uintx4 a;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          a[k] = __builtin_amdgcn_perm(word(k >> 1, 2 * (k & 1) + 1, 0, j >> 1), word(k >> 1, 2 * (k & 1), 0, j >> 1), j & 1 ? 0x07060302u : 0x05040100u);
-        into(j, [&](floatx4 c) __attribute__((always_inline)) {
-          return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, pb), c, 0, 0, 0);
-        });
+          a[k] = __builtin_amdgcn_perm(x.v[k >> 1][2 * (k & 1) + 1][0][j >> 1], x.v[k >> 1][2 * (k & 1)][0][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
+        o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, pb), o[j], 0, 0, 0);
       }
     } else {
 #pragma unroll
       for (int j = 0; j < J; ++j)
-        into(j, [&](floatx4 c) __attribute__((always_inline)) {
 #pragma unroll
-          for (int r = 0; r < 4; ++r) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(0, r, j / 4, j % 4)), pw[0][r], c, 0, 0, 0);
-          return c;
-        });
+        for (int r = 0; r < 4; ++r) o[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.v[0][r][j / 4][j % 4]), pw[0][r], o[j], 0, 0, 0);
     }
   };
   auto block = [&](const Block& x, int b) __attribute__((always_inline)) {
@@ -232,115 +233,102 @@ __global__ void __launch_bounds__(kPDecodeWaves * 64, 2) attn_pdecode_kernel(PAt
         s[t][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], p.scale_log2e, -ref));
         l_run += s[t][e];
       }
-    // Values that are not finite, of keys that some row does not see: 0 times them is not 0.  Each token's rows then take the block with the keys that
-    // they do not see as zeros.
-    bool odd = false;
-    if (__builtin_expect(masked && sq.n > 1, 0)) {
-#pragma unroll
-      for (int t = 0; t < TILES; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int j = 0; j < VV; ++j)
-#pragma unroll
-            for (int i = 0; i < VWORDS; ++i) {
-              const unsigned u = x.v[t][r][j][i];
-              if (BF16)
-                odd |= (u & 0x7f80u) == 0x7f80u || (u & 0x7f800000u) == 0x7f800000u;
-              else
-                odd |= (u & 0x7f800000u) == 0x7f800000u;
-            }
-      odd = __any(odd);
-    }
-    if (__builtin_expect(!odd, 1)) {
-      outputs(x, s, [&](int j, auto&& product) __attribute__((always_inline)) { o[j] = product(o[j]); }, 0, std::false_type{});
-    } else {
-#pragma unroll 1
-      for (int i = 0; i < sq.n; ++i)
-        outputs(
-            x, s,
-            [&](int j, auto&& product) __attribute__((always_inline)) {
-              const floatx4 part = product(floatx4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-              for (int r = 0; r < 4; ++r) o[j][r] += tok == i ? part[r] : 0.f;
-            },
-            prev + i + 1 - key0, std::true_type{});
-    }
+    outputs(x, s);
   };
 
-  Block x, y;
-  load(x, 0);
-  if (special) {
-    // ---- the block with new rows: what lies in the pages, zeros from there on, and the new rows in their stead, which are stored
-    const int key0 = b_last * BK;
-    y.gone = 0;
-#pragma unroll
-    for (int t = 0; t < TILES; ++t) {
-      const int key = key0 + 16 * t;
-      int page = -1;
-      if (key < sq.len) page = table[(unsigned)key >> p.page_log2];
-      load_tile(y, t, __builtin_amdgcn_readfirstlane(page), key);
-    }
-    auto place = [&](int key, uint64_t& at) __attribute__((always_inline)) -> bool {  // of the new row at this key in a layer's K, or V
-      const int64_t slot = p.slots[sq.first + key - prev];
-      at = (((uint64_t)slot >> p.page_log2) * p.page_bytes) + head + ((uint64_t)slot & ((1u << p.page_log2) - 1)) * ROWB;
-      return (uint64_t)slot < (uint64_t)p.n_places;
-    };
-    const int64_t new_row = p.kv_stride * (int64_t)sizeof(T);
-    const unsigned char* knew = static_cast<const unsigned char*>(p.k_new) + (int64_t)(sq.first - prev) * new_row + g * ROWB;
-    const unsigned char* vnew = static_cast<const unsigned char*>(p.v_new) + (int64_t)(sq.first - prev) * new_row + g * ROWB;
-#pragma unroll
-    for (int t = 0; t < TILES; ++t) {
-      const int key = key0 + 16 * t + c16;
-      if (key >= old && key < sq.len) {
-        uint64_t at;
-        const bool stored = place(key, at);
-#pragma unroll
-        for (int v = 0; v < KV; ++v) {
-          y.k[t][v] = *reinterpret_cast<const uintx4*>(knew + (int64_t)key * new_row + v * 64 + kg * 16);
-          if (stored) *reinterpret_cast<uintx4*>(static_cast<unsigned char*>(p.k_pages) + at + v * 64 + kg * 16) = y.k[t][v];
-        }
-      }
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int vkey = key0 + 16 * t + 4 * kg + r;
-        if (vkey >= old && vkey < sq.len) {
-          uint64_t at;
-          const bool stored = place(vkey, at);
-#pragma unroll
-          for (int j = 0; j < VV; ++j) {
-            const unsigned in_row = (unsigned)c16 * (VWORDS * 4) + j * 256;
-            y.v[t][r][j] = *reinterpret_cast<const vvec*>(vnew + (int64_t)vkey * new_row + in_row);
-            if (stored) *reinterpret_cast<vvec*>(static_cast<unsigned char*>(p.v_pages) + at + in_row) = y.v[t][r][j];
-          }
-        }
-      }
-    }
-    block(y, b_last);
-  }
-  if (n_plain > 0) {
-    int i = 0;
+  // Once; and where outputs are not finite, which may come from values that their rows do not see (0 times them is not 0), once more for each token, with what it does not
+  // see as zeros.
 #pragma unroll 1
-    while (true) {
-      load(y, i + 1);
-      block(x, b_first + NW * i);
-      if (++i >= n_plain) break;
-      load(x, i + 1);
-      block(y, b_first + NW * i);
-      if (++i >= n_plain) break;
+  for (int pass = -1; pass < sq.n; ++pass) {
+    if (pass >= 0) {
+      limit = prev + pass + 1;
+      fetch_pages(0, false);
     }
-  }
+    m_run = -INFINITY;
+    l_run = 0.f;
+#pragma unroll
+    for (int j = 0; j < J; ++j) o[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    Block x, y;
+    load(x, 0);
+    if (special) {
+      // ---- the block with new rows: what lies in the pages, zeros from there on, and the new rows in their stead, which are stored (16 bytes of a row's K or V a lane)
+      const int key0 = b_last * BK;
+      y.gone = 0;
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) {
+        const int key = key0 + 16 * t;
+        int page = __builtin_amdgcn_readlane(pages[t], (n_blocks - 1) & 63);
+        if (__builtin_expect(n_blocks > 64, 0)) {
+          page = -1;
+          if (key < sq.len) page = __builtin_amdgcn_readfirstlane(table[(unsigned)key >> p.page_log2]);
+        }
+        load_tile(y, t, page, key);
+      }
+      const int64_t new_row = p.kv_stride * (int64_t)sizeof(T);
+      const unsigned char* knew = static_cast<const unsigned char*>(p.k_new) + (int64_t)(sq.first - prev) * new_row + g * ROWB;
+      const unsigned char* vnew = static_cast<const unsigned char*>(p.v_new) + (int64_t)(sq.first - prev) * new_row + g * ROWB;
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) {
+        const int key = key0 + 16 * t + c16, vkey = key0 + 16 * t + 4 * kg;
+        if (y.gone >> t & 1) continue;  // (seen by nobody)
+        if (key >= old && key < limit)
+#pragma unroll
+          for (int v = 0; v < KV; ++v) y.k[t][v] = *reinterpret_cast<const uintx4*>(knew + (int64_t)key * new_row + v * 64 + kg * 16);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (vkey + r >= old && vkey + r < limit)
+#pragma unroll
+            for (int v = 0; v < VV; ++v)
+              y.v[t][r][v] = *reinterpret_cast<const vvec*>(vnew + (int64_t)(vkey + r) * new_row + (unsigned)c16 * (VWORDS * 4) + v * 256);
+      }
+      constexpr int CH = ROWB / 16;
+      const int from = old > key0 ? old : key0, to = key0 + BK < sq.len ? key0 + BK : sq.len;
+#pragma unroll 1
+      for (int e = l; pass < 0 && e < (to - from) * (2 * CH); e += 64) {
+        const int key = from + e / (2 * CH), c = e % CH * 16;
+        const bool is_v = e / CH & 1;
+        const int64_t slot = p.slots[sq.first + key - prev];
+        const uintx4 row16 = *reinterpret_cast<const uintx4*>((is_v ? vnew : knew) + (int64_t)key * new_row + c);
+        const uint64_t at = ((uint64_t)slot >> p.page_log2) * p.page_bytes + head + ((uint64_t)slot & ((1u << p.page_log2) - 1)) * ROWB + (unsigned)c;
+        if ((uint64_t)slot < (uint64_t)p.n_places) *reinterpret_cast<uintx4*>(static_cast<unsigned char*>(is_v ? p.v_pages : p.k_pages) + at) = row16;
+      }
+      block(y, b_last);
+    }
+    if (n_plain > 0) {
+      int i = 0;
+#pragma unroll 1
+      while (true) {
+        load(y, i + 1);
+        asm volatile("" ::: "memory");
+        block(x, b_first + NW * i);
+        if (++i >= n_plain) break;
+        load(x, i + 1);
+        asm volatile("" ::: "memory");
+        block(y, b_first + NW * i);
+        if (++i >= n_plain) break;
+      }
+    }
 
-  // ---- the wavefronts' results meet in LDS: [wavefront][row][D] and [wavefront][row] (m, l)
-  const float l_tot = pair_sum(row16_sum(l_run));
-  if (c16 < rows) {
-    float* mine = reinterpret_cast<float*>(red_o + (w * ROWS + c16) * OROW);
+    // ---- the wavefronts' results meet in LDS: [wavefront][row][D] and [wavefront][row] (m, l)
+    const float l_tot = pair_sum(row16_sum(l_run));
+    if (c16 < rows && (pass < 0 || tok == pass)) {
+      float* mine = reinterpret_cast<float*>(red_o + (w * ROWS + c16) * OROW);
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+      for (int r = 0; r < 4; ++r)
 #pragma unroll
-      for (int j = 0; j < J; j += 4)  // columns CW m + j of share 0, or 64 (j / 4) + 4 m + j % 4, m = 4 kg + r
-        *reinterpret_cast<floatx4*>(mine + (BF16 ? CW * (4 * kg + r) + j : 16 * j + 4 * (4 * kg + r))) = floatx4{o[j][r], o[j + 1][r], o[j + 2][r], o[j + 3][r]};
-    if (kg == 0) red_ml[w * ROWS + c16] = floatx2{m_run, l_tot};
+        for (int j = 0; j < J; j += 4)  // columns CW m + j of share 0, or 64 (j / 4) + 4 m + j % 4, m = 4 kg + r
+          *reinterpret_cast<floatx4*>(mine + (BF16 ? CW * (4 * kg + r) + j : 16 * j + 4 * (4 * kg + r))) = floatx4{o[j][r], o[j + 1][r], o[j + 2][r], o[j + 3][r]};
+      if (kg == 0) red_ml[w * ROWS + c16] = floatx2{m_run, l_tot};
+    }
+    if (pass < 0) {
+      if (sq.n == 1) break;
+      float check = 0.f;  // (0 as long as all are finite)
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) check = __builtin_fmaf(o[j][r], 0.f, check);
+      if (__builtin_expect(!__any(check != 0.f), 1)) break;
+    }
   }
   __syncthreads();
 

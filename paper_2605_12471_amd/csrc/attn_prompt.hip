@@ -262,7 +262,7 @@ __global__ void __launch_bounds__(256, 1) attn_prompt_kernel(PAttnParams p) {
 
   const int tid = threadIdx.x, l = tid & 63, hi = l >> 5, m = l & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const PromptWork wk = prompt_work(p, blockIdx.x, l);
+  const PromptWork wk = prompt_work(p, blockIdx.x);
   if (!wk.any) return;
   // The lane, found again where it is rarely needed, not held through the main loop
   auto lane_now = []() __attribute__((always_inline)) -> int {
@@ -1066,7 +1066,7 @@ __global__ void __launch_bounds__(256, 2) attn_prompt_few_kernel(PAttnParams p) 
 
   const int tid = threadIdx.x, l = tid & 63, h = l >> 5, c32 = l & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const PromptWork wk = prompt_work(p, blockIdx.x, l);
+  const PromptWork wk = prompt_work(p, blockIdx.x);
   if (!wk.any) return;
   const int prev = wk.sq.len - wk.sq.n;
 
@@ -1253,7 +1253,7 @@ static hipError_t prepare_both() {
 }
 template <int D>
 static hipError_t launch_one(const PAttnParams& p, int units_per_wave, hipStream_t s) {
-  const dim3 grid((unsigned)p.n_units * (unsigned)p.n_pieces * (unsigned)p.n_kv_heads), block(256);
+  const dim3 grid((unsigned)p.n_units * (unsigned)p.n_kv_heads), block(256);
   if (units_per_wave == 2)
     hipLaunchKernelGGL(attn_prompt_kernel<D>, grid, block, prompt_lds<D>, s, p);
   else
@@ -1268,12 +1268,18 @@ hipError_t launch_attn_prompt(const PAttnParams& p, int head_dim, bool bf16, int
 
 // ---- the merge of pieces ---------------------------------------------------------------------------------------------------
 // A thread has 16 bytes of a row and goes through its pieces, eight in flight; rows of one piece have been written.  Bound by memory.
+constexpr int kMergeRows = 32;  // of a workgroup
 template <class T, int D>
 __global__ void __launch_bounds__(256) pmerge_kernel(PAttnParams p, int parts_log2) {
-  constexpr int V = D / 4, ROWS = 256 / V;  // (rows of a workgroup: unit_rows / ROWS = 2^parts_log2 of them share a block's)
-  const PromptWork wk = prompt_work(p, blockIdx.x >> parts_log2, threadIdx.x & 63);
-  const int c = threadIdx.x % V, r = wk.row0 + (int)(blockIdx.x & ((1u << parts_log2) - 1)) * ROWS + threadIdx.x / V, n = wk.n_pieces;
-  if (!wk.any || n < 2 || r >= wk.rows) return;
+  constexpr int V = D / 4, ROWS = 256 / V;  // (unit_rows / kMergeRows = 2^parts_log2 workgroups share a block's rows)
+  const unsigned id = blockIdx.x >> parts_log2;
+  const int at_block = (int)quot(id, p.by_kv_heads);
+  if (at_block >= ((ConstPtr<int32_t>)(uintptr_t)p.list_head)[1]) return;
+  const PromptWork wk = prompt_item(p, ((ConstPtr<int32_t>)(uintptr_t)p.merges)[at_block], (int)id - at_block * p.n_kv_heads);
+  const int n = wk.n_pieces;
+  const int c = threadIdx.x % V, first = wk.row0 + (int)(blockIdx.x & ((1u << parts_log2) - 1)) * kMergeRows;
+#pragma unroll 1
+  for (int r = first + threadIdx.x / V; r < first + kMergeRows && r < wk.rows; r += ROWS) {
   const int tok = (int)quot((unsigned)r, p.by_group), head = wk.g * p.group + r - tok * p.group;
   const int64_t n_rows = (int64_t)p.n_tokens * p.n_q_heads, token = wk.sq.first + tok, at = token * p.n_q_heads + head;
   float M = -INFINITY, L = 0.f;
@@ -1323,12 +1329,13 @@ __global__ void __launch_bounds__(256) pmerge_kernel(PAttnParams p, int parts_lo
     *reinterpret_cast<floatx4*>(static_cast<float*>(p.out) + at * D + c * 4) = acc;
   }
   if (p.lse && c == 0) p.lse[(int64_t)head * p.n_tokens + token] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * 0.6931471805599453f;
+  }
 }
 
 hipError_t launch_pmerge(const PAttnParams& p, int head_dim, bool bf16, hipStream_t s) {
   int lg = 0;
-  while ((256 / (head_dim / 4)) << lg < p.unit_rows) ++lg;
-  const dim3 grid(((unsigned)p.n_units * (unsigned)p.n_kv_heads) << lg), block(256);
+  while (kMergeRows << lg < p.unit_rows) ++lg;
+  const dim3 grid(((unsigned)p.n_blocks * (unsigned)p.n_kv_heads) << lg), block(256);
   if (bf16 && head_dim == 128)
     hipLaunchKernelGGL((pmerge_kernel<__bf16, 128>), grid, block, 0, s, p, lg);
   else if (bf16)

@@ -12,12 +12,12 @@ typedef __attribute__((ext_vector_type(16))) float floatx16;
 typedef __attribute__((ext_vector_type(4))) float floatx4;
 typedef __attribute__((ext_vector_type(2))) float floatx2;
 
-constexpr int kF32Ring = 3, kF32Tile = 32;
+constexpr int kF32Ring = 2, kF32Tile = 32;
 template <int D>
 constexpr int prompt_f32_lds = kF32Ring * 2 * kF32Tile * D * 4;
 
 template <int D>
-__global__ void __launch_bounds__(256, 1) attn_prompt_f32_kernel(PAttnParams p) {
+__global__ void __launch_bounds__(256, 2) attn_prompt_f32_kernel(PAttnParams p) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const unsigned lds0 = (unsigned)(uintptr_t)((unsigned char __attribute__((address_space(3)))*)smem);
   constexpr int CH = D / 4, ROWB = D * 4, KS = D / 8, JT = D / 32;  // 16-byte chunks and bytes of a row; 16-byte shares of a lane; tiles of O^T
@@ -28,7 +28,7 @@ __global__ void __launch_bounds__(256, 1) attn_prompt_f32_kernel(PAttnParams p) 
 
   const int tid = threadIdx.x, l = tid & 63, h = l >> 5, c32 = l & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const PromptWork wk = prompt_work(p, blockIdx.x, l);
+  const PromptWork wk = prompt_work(p, blockIdx.x);
   if (!wk.any) return;
   const int G = p.group, Hq = p.n_q_heads, prev = wk.sq.len - wk.sq.n;
 
@@ -59,8 +59,8 @@ __global__ void __launch_bounds__(256, 1) attn_prompt_f32_kernel(PAttnParams p) 
     k_off[i] = (unsigned)(r * ROWB + (((l % CH) ^ (in_tile % 16)) * 16));
   }
   const unsigned v_off = (unsigned)(l * 16);
-  auto issue = [&](int t) __attribute__((always_inline)) -> bool {
-    if (t >= t_end) return false;
+  auto issue = [&](int t) __attribute__((always_inline)) {
+    if (t >= t_end) return;
     if ((t & 31) == 0 || t == t_begin) win.fetch(p, table, (t & ~31) * BN, wk.sq.len, l);
     const int at = 2 * (t & 31) + (w >> 1), key0 = t * BN + 8 * w;
     const int number = __builtin_amdgcn_readlane(win.number, at);
@@ -74,7 +74,7 @@ __global__ void __launch_bounds__(256, 1) attn_prompt_f32_kernel(PAttnParams p) 
         dma16(kf, k_off[i], slot + i * 1024);
         dma16(vf, v_off + i * 1024, slot + TILEB + i * 1024);
       }
-      return true;
+      return;
     }
     const int n = there ? wk.sq.len - key0 : 0;  // rows that are not there become zeros
 #pragma unroll
@@ -87,16 +87,20 @@ __global__ void __launch_bounds__(256, 1) attn_prompt_f32_kernel(PAttnParams p) 
         *LDS_PTR(floatx4, slot + (unsigned)(TILEB + i * 1024 + l * 16)) = floatx4{0.f, 0.f, 0.f, 0.f};
       }
     }
-    return false;
   };
 
   const unsigned krow = lds0 + (unsigned)(c32 * ROWB), vrow = lds0 + (unsigned)(TILEB + 4 * h * ROWB + c32 * (JT * 4));
-  floatx16 o[JT];
-  float m_run, l_run;
   constexpr floatx16 zero = {};
-
-  auto attend = [&](int t, uint64_t gone, bool careful) __attribute__((always_inline)) {
+  auto barrier = [&]() __attribute__((always_inline)) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  // A tile's S^T, masked; then the reference of a row, and what a row's results are to be multiplied by (1 but for a wavefront that moves one); then weights, and their sum
+  auto logits = [&](int t) __attribute__((always_inline)) -> floatx16 {
     const unsigned slot = (unsigned)((t % NS) * 2 * TILEB);
+    const uint64_t gone = ~win.there >> (2 * (t & 31)) & 3;  // of the tile's two runs of 16 keys, those of no page
+    issue(t + 1);
     floatx16 s = zero;
 #pragma unroll
     for (int j = 0; j < KS; ++j) {
@@ -110,114 +114,150 @@ __global__ void __launch_bounds__(256, 1) attn_prompt_f32_kernel(PAttnParams p) 
       for (int i = 0; i < 16; ++i)
         if (8 * (i >> 2) + (i & 3) >= rel || (gone >> (i >> 3) & 1)) s[i] = -INFINITY;
     }
+    return s;
+  };
+  auto reference = [&](const floatx16& s, float& m_run, float& alpha) __attribute__((always_inline)) -> bool {
     float mx = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[i]);
     mx = pair_max(mx) * p.scale_log2e;
+    // only rows that ask for it move, so a row's arithmetic never depends on its wave neighbours
     const bool mine = mx > m_run + kStale || (m_run == -INFINITY && mx > -INFINITY);
-    if (__any(mine)) {
-      const float m2 = mine ? mx : m_run;
-      const float alpha = m_run == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m2);
-      m_run = m2;
+    if (!__any(mine)) return false;
+    const float m2 = mine ? mx : m_run;
+    alpha = m_run == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m2);
+    m_run = m2;
+    return true;
+  };
+  auto weights = [&](floatx16& s, float m_run) __attribute__((always_inline)) -> float {
+    const float ref = m_run == -INFINITY ? 0.f : m_run;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], p.scale_log2e, -ref));
+      sum += s[i];
+    }
+    return sum;
+  };
+
+#pragma unroll
+  for (int j = 0; j < KS; ++j) asm volatile("" : "+v"(qf[j]));  // (waited for here, not in the loop)
+  floatx16 o[JT];
+  float m_run = -INFINITY, l_run = 0.f;
+#pragma unroll
+  for (int j = 0; j < JT; ++j) o[j] = zero;
+  issue(t_begin);
+#pragma unroll 1
+  for (int t = t_begin; t < t_end; ++t) {
+    wait_vm<0>();
+    barrier();  // the tile is there for all, and the slot of the one before is free
+    if (t * BN >= vis_last) {
+      issue(t + 1);
+      continue;
+    }
+    floatx16 s = logits(t);
+    float alpha;
+    if (reference(s, m_run, alpha)) {
       l_run *= alpha;
 #pragma unroll
       for (int j = 0; j < JT; ++j)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[j][i] *= alpha;
     }
-    const float ref = m_run == -INFINITY ? 0.f : m_run;
+    l_run += weights(s, m_run);
+    const unsigned at = vrow + (unsigned)((t % NS) * 2 * TILEB);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], p.scale_log2e, -ref));
-      l_run += s[i];
+      const vvec v = *LDS_PTR(const vvec, at + (unsigned)((8 * (i >> 2) + (i & 3)) * ROWB));
+#pragma unroll
+      for (int j = 0; j < JT; ++j) o[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[j], s[i], o[j], 0, 0, 0);
     }
+  }
+
+  // ---- out, or what the piece leaves for the merge
+  const int r = unit0 + c32;
+  const bool alone = wk.n_pieces == 1;
+  int64_t at = 0, part = 0;
+  int head_q = 0, tok_out = 0;
+  if (r < wk.rows) {
+    tok_out = (int)quot((unsigned)r, p.by_group);
+    head_q = wk.g * G + r - tok_out * G;
+    at = (int64_t)(wk.sq.first + tok_out) * Hq + head_q;
+    part = (int64_t)wk.piece * p.n_tokens * Hq + at;
+  }
+  auto sums = [&](float m, float l_tot) __attribute__((always_inline)) {
+    if (h || r >= wk.rows) return;
+    if (!alone)
+      *reinterpret_cast<floatx2*>(p.part_ml + part * 2) = floatx2{m, l_tot};
+    else if (p.lse)
+      p.lse[(int64_t)head_q * p.n_tokens + wk.sq.first + tok_out] = l_tot == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l_tot)) * 0.6931471805599453f;
+  };
+  float* out = (alone ? static_cast<float*>(p.out) + at * D : p.part_o + part * D) + 4 * h * JT;
+  float check = 0.f;  // 0 as long as all outputs are finite
+  {
+    const float l_tot = pair_sum(l_run), inv = !alone ? 1.f : l_tot == 0.f ? 0.f : 1.f / l_tot;
+    sums(m_run, l_tot);
+    if (r < wk.rows) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      vvec v = *LDS_PTR(const vvec, vrow + slot + (unsigned)((8 * (i >> 2) + (i & 3)) * ROWB));
-      if (__builtin_expect(!careful, 1)) {
-#pragma unroll
-        for (int j = 0; j < JT; ++j) o[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[j], s[i], o[j], 0, 0, 0);
-      } else {
-        // (values that are not finite, of keys that some rows do not see: rows that see the first of the two keys alone take the other's as zeros, rows that
-        // see neither take nothing)
-        const int sees = my_vis - key0 - (8 * (i >> 2) + (i & 3));
+      for (int i = 0; i < 16; ++i) {
+        vvec v;
 #pragma unroll
         for (int j = 0; j < JT; ++j) {
-          const floatx16 both = __builtin_amdgcn_mfma_f32_32x32x2f32(v[j], s[i], zero, 0, 0, 0);
-          const floatx16 one = __builtin_amdgcn_mfma_f32_32x32x2f32(h ? 0.f : v[j], s[i], zero, 0, 0, 0);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[j][e] += sees > 4 ? both[e] : sees > 0 ? one[e] : 0.f;
+          check = __builtin_fmaf(o[j][i], 0.f, check);
+          v[j] = o[j][i] * inv;
         }
+        *reinterpret_cast<vvec*>(out + (8 * (i >> 2) + (i & 3)) * JT) = v;
       }
     }
-  };
-
-  auto barrier = [&]() __attribute__((always_inline)) {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-  };
+  }
+  // Outputs that are not finite may come from values that their rows do not see (0 times them is not 0): everything once more, then, a tile of O^T at a time; of a
+  // step's two keys, rows that see the first alone take the other's values as zeros, rows that see neither take nothing.
+  wait_vm<0>();
+  __syncthreads();
+  const int vote = __any(check != 0.f) ? 1 : 0;  // (NaN)
+  if (l == 0) *LDS_PTR(int, lds0 + 4 * w) = vote;
+  __syncthreads();
+  int again = 0;
 #pragma unroll
-  for (int j = 0; j < KS; ++j) asm volatile("" : "+v"(qf[j]));  // (waited for here, not in the loop)
+  for (int i = 0; i < 4; ++i) again |= *LDS_PTR(const int, lds0 + 4 * i);
+  if (__builtin_expect(__builtin_amdgcn_readfirstlane(again) == 0, 1)) return;
 #pragma unroll 1
-  for (bool careful = false;; careful = true) {
-    m_run = -INFINITY;
-    l_run = 0.f;
-#pragma unroll
-    for (int j = 0; j < JT; ++j) o[j] = zero;
+  for (int j = 0; j < JT; ++j) {
+    floatx16 acc = zero;
+    float m = -INFINITY, total = 0.f;
+    __syncthreads();
     issue(t_begin);
-    uint64_t gone = ~win.there >> (2 * (t_begin & 31)) & 3;
-    bool ahead = issue(t_begin + 1);
 #pragma unroll 1
     for (int t = t_begin; t < t_end; ++t) {
-      const uint64_t gone_next = ~win.there >> (2 * ((t + 1) & 31)) & 3;
-      if (ahead)
-        wait_vm<2 * SLABS>();
-      else
-        wait_vm<0>();
+      wait_vm<0>();
       barrier();
-      ahead = issue(t + 2);
-      if (t * BN < vis_last) attend(t, gone, careful);
-      gone = gone_next;
+      floatx16 s = logits(t);
+      float alpha;
+      if (reference(s, m, alpha)) {
+        total *= alpha;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[i] *= alpha;
+      }
+      total += weights(s, m);
+      const unsigned from = vrow + (unsigned)((t % NS) * 2 * TILEB + j * 4);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int k0 = 8 * (i >> 2) + (i & 3), sees = my_vis - t * BN - k0;
+        const float v = *LDS_PTR(const float, from + (unsigned)(k0 * ROWB));
+        floatx16 x = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[i], zero, 0, 0, 0);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[e] += sees > 4 ? x[e] : 0.f;
+        x = __builtin_amdgcn_mfma_f32_32x32x2f32(h ? 0.f : v, s[i], zero, 0, 0, 0);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[e] += sees > 0 && sees <= 4 ? x[e] : 0.f;
+      }
     }
-    bool odd = false;
+    const float l_tot = pair_sum(total), inv = !alone ? 1.f : l_tot == 0.f ? 0.f : 1.f / l_tot;
+    if (j == 0) sums(m, l_tot);
+    if (r < wk.rows) {
 #pragma unroll
-    for (int j = 0; j < JT; ++j)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) odd |= !(__builtin_fabsf(o[j][i]) < INFINITY);
-    wait_vm<0>();
-    barrier();
-    if (careful) break;
-    const int mine = __any(odd) ? 1 : 0;
-    if (l == 0) *LDS_PTR(int, lds0 + 4 * w) = mine;
-    barrier();
-    int again = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) again |= *LDS_PTR(const int, lds0 + 4 * i);
-    barrier();
-    if (!__builtin_amdgcn_readfirstlane(again)) break;
-  }
-
-  const float l_tot = pair_sum(l_run);
-  const int r = unit0 + c32;
-  if (r >= wk.rows) return;
-  const int t = (int)quot((unsigned)r, p.by_group), head_q = wk.g * G + r - t * G;
-  const int64_t at = (int64_t)(wk.sq.first + t) * Hq + head_q, part = (int64_t)wk.piece * p.n_tokens * Hq + at;
-  const bool alone = wk.n_pieces == 1;
-  const float inv = !alone ? 1.f : l_tot == 0.f ? 0.f : 1.f / l_tot;
-  float* out = (alone ? static_cast<float*>(p.out) + at * D : p.part_o + part * D) + 4 * h * JT;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    vvec v;
-#pragma unroll
-    for (int j = 0; j < JT; ++j) v[j] = alone && l_tot == 0.f ? 0.f : o[j][i] * inv;
-    *reinterpret_cast<vvec*>(out + (8 * (i >> 2) + (i & 3)) * JT) = v;
-  }
-  if (h == 0) {
-    if (!alone)
-      *reinterpret_cast<floatx2*>(p.part_ml + part * 2) = floatx2{m_run, l_tot};
-    else if (p.lse)
-      p.lse[(int64_t)head_q * p.n_tokens + wk.sq.first + t] = l_tot == 0.f ? -INFINITY : (m_run + __builtin_amdgcn_logf(l_tot)) * 0.6931471805599453f;
+      for (int i = 0; i < 16; ++i) out[(8 * (i >> 2) + (i & 3)) * JT + j] = acc[i] * inv;
+    }
   }
 }
 
@@ -236,7 +276,7 @@ static hipError_t prepare_one() {
 hipError_t prepare_attn_prompt_f32(int head_dim) { return head_dim == 128 ? prepare_one<128>() : prepare_one<64>(); }
 
 hipError_t launch_attn_prompt_f32(const PAttnParams& p, int head_dim, hipStream_t s) {
-  const dim3 grid((unsigned)p.n_units * (unsigned)p.n_pieces * (unsigned)p.n_kv_heads), block(256);
+  const dim3 grid((unsigned)p.n_units * (unsigned)p.n_kv_heads), block(256);
   if (head_dim == 128)
     hipLaunchKernelGGL(attn_prompt_f32_kernel<128>, grid, block, prompt_f32_lds<128>, s, p);
   else

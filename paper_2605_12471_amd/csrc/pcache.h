@@ -21,18 +21,30 @@ struct PagedPlan {
   bool decode;           // at most 16 packed rows per sequence and KV head: the kernel that deals keys to wavefronts
   int unit_rows;         // packed rows of a workgroup (decode: of a sequence and KV head)
   int units_per_wave;    // prompts: 32-row units of a wavefront
-  int64_t blocks;        // prompts: workgroups per KV head and piece, an upper bound of those with rows
+  bool from_end;         // decode: a sequence's last piece is whole, and its first what is left
+  int64_t blocks, items;  // prompts: blocks of rows per KV head, and these with a piece of their keys each, at most
+  int places, shares, shortest, cost_once, cost_split;  // PromptPlanParams
   int n_pieces;          // of the keys, at most
-  int piece;             // keys of one, a multiple of 128
+  int piece;             // decode: keys of one, a multiple of 128
   int64_t rows;          // of partial results
-  size_t counters;       // bytes in front of them, of the counters by which pieces meet
+  size_t counters;       // bytes in front of them: of the counters by which pieces meet,
+  size_t list;           // prompts: and of the work's list
   size_t bytes;          // of the workspace
 };
 PagedPlan make_pplan(const kvfold_pcache_config_t& c, int n_cu, const kvfold_batch_t& b);
 
-// Prompts: the workgroups of sequence s, whose new tokens are first .. first + n - 1 of the packed ones, are numbered from here on; each has unit_rows packed rows
-// of the sequence.  (For any first tokens that ascend: floor(a + x) - floor(a) + 1 >= ceil(x), so that the numbers of two sequences never meet.)
-KVFOLD_HD int64_t paged_first_block(int64_t first, int s, int G, int unit_rows) { return first * G / unit_rows + s; }
+// Prompts: a block of rows of a sequence and a piece of the keys that its last row sees.  The list of them is made on the device, from the lengths there, in front of the
+// attention (pcache_rows.hip); its head says how many there are.
+struct PromptItem {
+  int32_t seq, first, n, len;  // the sequence, its new tokens among the packed ones, its length
+  int32_t row0;                // the block's first packed (token, query head) row
+  int32_t key_begin, key_end;  // the piece
+  int32_t piece;               // its number, and how many the block has in all << 16
+};
+static_assert(sizeof(PromptItem) == 32, "an item is fetched at once");
+constexpr int kPromptHead = 64;     // bytes in front of the list: the number of items, of blocks to merge, and the keys of a piece
+constexpr int kPromptShares = 6;    // pieces are no shorter than this part of a place's share of the work
+constexpr int kPromptMaxPieces = 64;
 
 // The pieces of `len` keys, one at least
 KVFOLD_HD int paged_pieces(int len, int piece) {
@@ -70,6 +82,15 @@ struct AssignParams {
 };
 hipError_t launch_assign(const AssignParams& p, int n_cu, hipStream_t s);
 
+// The list of a batch's work, made by one workgroup
+struct PromptPlanParams {
+  const int32_t *lens, *cu_new;
+  int32_t* head;      // [0] items, [1] blocks to merge, [2] keys of a piece
+  PromptItem* items;  // nullptr: no list is asked for
+  int32_t* merges;    // behind them: the first pieces of blocks that have several
+  int32_t n_seqs, n_tokens, max_new, max_len, group, unit_rows, max_items, n_pieces, n_kv_heads;
+  int32_t n_places, n_shares, shortest, cost_once, cost_split;  // workgroups that the GPU has room for; of pieces, in tiles; and what one costs, also in tiles
+};
 struct PAppendParams {
   const void *k, *v;  // [n_tokens][Hkv][d] at token_bytes
   void *k_pages, *v_pages;
@@ -78,7 +99,7 @@ struct PAppendParams {
   int64_t n_places;
   int32_t n_tokens, n_kv_heads, row_bytes, page_log2;
 };
-hipError_t launch_pappend(const PAppendParams& p, hipStream_t s);
+hipError_t launch_pappend(const PAppendParams& p, const PromptPlanParams& plan, hipStream_t s);
 
 struct PAttnParams {
   const void* q;
@@ -90,13 +111,18 @@ struct PAttnParams {
   const int64_t* slots;
   uint32_t* counters;  // zero between steps
   float *part_o, *part_ml;
+  const int32_t* list_head;  // prompts
+  const PromptItem* items;
+  const int32_t* merges;
   int64_t table_stride, q_stride, kv_stride;  // (the latter two in elements)
   int64_t n_places;
   uint64_t page_bytes;  // of K or V of a page
   int32_t n_seqs, n_tokens, max_new, max_len;  // (max_len: also what a row of the tables can name)
   int32_t n_q_heads, n_kv_heads, group, page_log2, n_pages;
   int32_t n_pieces, piece, unit_rows;
-  int32_t n_units;  // decode: sequences times KV heads; prompts: blocks
+  int32_t n_units;   // decode: sequences times KV heads; prompts: items at most
+  int32_t n_blocks;  // prompts: blocks of rows, at most
+  int32_t from_end;  // decode: PagedPlan
   float scale_log2e, from_log2, stale;  // its reciprocal, and 2^16 in its units
   FastDiv by_group, by_units, by_kv_heads;
 };

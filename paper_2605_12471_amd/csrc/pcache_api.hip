@@ -38,7 +38,8 @@ bool all_apart(const Range& a, const Range* others, int n) {
 // Bytes of n tokens' rows of `heads` heads at `stride` elements
 size_t extent(int64_t n, int64_t stride, int64_t heads, int64_t d, int es) { return n < 1 ? 0 : ((size_t)(n - 1) * (size_t)stride + (size_t)(heads * d)) * (size_t)es; }
 
-hipError_t append_rows(const kvfold_pcache* c, int layer, const void* k, const void* v, int64_t kv_stride, const int64_t* slots, int32_t n, hipStream_t s) {
+hipError_t append_rows(const kvfold_pcache* c, int layer, const void* k, const void* v, int64_t kv_stride, const int64_t* slots, int32_t n, const PromptPlanParams& plan,
+                       hipStream_t s) {
   PAppendParams p;
   p.k = k;
   p.v = v;
@@ -51,7 +52,7 @@ hipError_t append_rows(const kvfold_pcache* c, int layer, const void* k, const v
   p.n_kv_heads = c->cfg.n_kv_heads;
   p.row_bytes = c->cfg.head_dim * c->es();
   p.page_log2 = c->page_log2;
-  return launch_pappend(p, s);
+  return launch_pappend(p, plan, s);
 }
 
 }  // namespace
@@ -176,7 +177,7 @@ int kvfold_pcache_append(const kvfold_pcache_t* c, int layer, const void* k, con
   if (!all_apart({c->store, c->bytes()}, inputs, 3)) return KVFOLD_ERR_INVALID_ARG;
   DeviceGuard guard(c->cfg.device);
   if (guard.err != hipSuccess) return hip_fail(guard.err);
-  const hipError_t e = append_rows(c, layer, k, v, stride, slots, n_tokens, static_cast<hipStream_t>(stream));
+  const hipError_t e = append_rows(c, layer, k, v, stride, slots, n_tokens, PromptPlanParams{}, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? KVFOLD_OK : hip_fail(e);
 }
 
@@ -224,7 +225,13 @@ int kvfold_pcache_step(const kvfold_pcache_t* c, int layer, const kvfold_batch_t
   p.cu_new = b->cu_new;
   p.slots = b->slots;
   p.counters = static_cast<uint32_t*>(workspace);
-  p.part_o = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + pl.counters);
+  unsigned char* list = static_cast<unsigned char*>(workspace) + pl.counters;
+  p.list_head = reinterpret_cast<int32_t*>(list);
+  p.items = reinterpret_cast<PromptItem*>(list + kPromptHead);
+  p.merges = reinterpret_cast<int32_t*>(list + kPromptHead + (size_t)pl.items * sizeof(PromptItem));
+  p.n_blocks = (int32_t)pl.blocks;
+  p.from_end = pl.from_end;
+  p.part_o = reinterpret_cast<float*>(list + pl.list);
   p.part_ml = p.part_o + pl.rows * f.head_dim;
   p.table_stride = b->table_stride;
   p.q_stride = q_stride;
@@ -244,7 +251,7 @@ int kvfold_pcache_step(const kvfold_pcache_t* c, int layer, const kvfold_batch_t
   p.n_pieces = pl.n_pieces;
   p.piece = pl.piece;
   p.unit_rows = pl.unit_rows;
-  p.n_units = pl.decode ? b->n_seqs * f.n_kv_heads : (int32_t)pl.blocks;
+  p.n_units = pl.decode ? b->n_seqs * f.n_kv_heads : (int32_t)pl.items;
   p.scale_log2e = c->scale * 1.4426950408889634f;
   p.from_log2 = 1.0f / p.scale_log2e;
   p.stale = 16.0f * p.from_log2;
@@ -255,7 +262,27 @@ int kvfold_pcache_step(const kvfold_pcache_t* c, int layer, const kvfold_batch_t
   if (pl.decode) {
     e = launch_attn_pdecode(p, f.head_dim, bf16, s);
   } else {
-    e = fresh ? append_rows(c, layer, k_new, v_new, kv_stride, b->slots, b->n_tokens, s) : hipSuccess;
+    PromptPlanParams plan;
+    plan.lens = b->lens;
+    plan.cu_new = b->cu_new;
+    plan.head = reinterpret_cast<int32_t*>(list);
+    plan.items = reinterpret_cast<PromptItem*>(list + kPromptHead);
+    plan.n_seqs = b->n_seqs;
+    plan.n_tokens = b->n_tokens;
+    plan.max_new = p.max_new;
+    plan.max_len = p.max_len;
+    plan.group = p.group;
+    plan.unit_rows = pl.unit_rows;
+    plan.max_items = (int32_t)pl.items;
+    plan.n_pieces = pl.n_pieces;
+    plan.n_kv_heads = f.n_kv_heads;
+    plan.merges = const_cast<int32_t*>(p.merges);
+    plan.n_places = pl.places;
+    plan.n_shares = pl.shares;
+    plan.shortest = pl.shortest;
+    plan.cost_once = pl.cost_once;
+    plan.cost_split = pl.cost_split;
+    e = append_rows(c, layer, k_new, v_new, kv_stride, b->slots, fresh ? b->n_tokens : 0, plan, s);
     if (e == hipSuccess) e = launch_attn_prompt(p, f.head_dim, bf16, pl.units_per_wave, s);
     if (e == hipSuccess && pl.n_pieces > 1) e = launch_pmerge(p, f.head_dim, bf16, s);
   }

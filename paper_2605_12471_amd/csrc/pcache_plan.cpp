@@ -49,26 +49,41 @@ PagedPlan make_pplan(const kvfold_pcache_config_t& c, int n_cu, const kvfold_bat
   if (pl.decode) {
     pl.unit_rows = (int)max_new * G;
     pl.units_per_wave = 1;
-    pieces = std::max((2 * n_cu + units - 1) / units, (len + 2047) / 2048);
+    // Where pieces are many the whole ones come first, else the way to the first keys counts (attn_pdecode.hip)
+    pl.from_end = units >= n_cu;
+    pieces = std::max((n_cu + units - 1) / units, (len + 2047) / 2048);
     pieces = std::min(pieces, kPagedMaxRows / (units * pl.unit_rows));
     pieces = std::max<int64_t>(1, std::min<int64_t>({pieces, steps, kPagedMaxPieces}));
     pl.piece = (int)((steps + pieces - 1) / pieces) * 128;
     pl.n_pieces = paged_pieces((int)len, pl.piece);
     pl.rows = pl.n_pieces > 1 ? units * pl.n_pieces * pl.unit_rows : 0;
   } else {
-    pl.units_per_wave = c.dtype == KVFOLD_BF16 && (int64_t)b.n_tokens * G >= (int64_t)b.n_seqs * 192 ? 2 : 1;
+    const int64_t rows_a_seq = (int64_t)b.n_tokens * G / std::max(b.n_seqs, 1);
+    const bool bf16 = c.dtype == KVFOLD_BF16;
+    pl.units_per_wave = bf16 && rows_a_seq > 128 && len > 1024 ? 2 : 1;
     pl.unit_rows = kUnitsPerWg * kRowsPerUnit * pl.units_per_wave;
-    pl.blocks = (int64_t)b.n_tokens * G / pl.unit_rows + b.n_seqs;
-    const int64_t rows = (int64_t)b.n_tokens * c.n_q_heads, wgs = std::max<int64_t>(1, ((int64_t)b.n_tokens * G + pl.unit_rows - 1) / pl.unit_rows * c.n_kv_heads);
-    pieces = std::max<int64_t>(1, 2 * n_cu / wgs);
-    pieces = std::min(pieces, kPagedMaxRows / std::max<int64_t>(rows, 1));
-    pieces = std::max<int64_t>(1, std::min<int64_t>({pieces, steps, 16}));
-    pl.piece = (int)((steps + pieces - 1) / pieces) * 128;
-    pl.n_pieces = paged_pieces((int)len, pl.piece);
+    // Blocks of rows: a sequence's last one is filled up.  Pieces: no shorter than a part of a CU's share of all tiles (pcache_rows.hip), so that there are at
+    // most so many more of them.
+    pl.blocks = (int64_t)b.n_tokens * G / pl.unit_rows + std::min<int64_t>(b.n_seqs, b.n_tokens);
+    pl.places = pl.units_per_wave == 2 ? n_cu : 2 * n_cu;
+    pl.shortest = bf16 ? 4 : 2;
+    pl.cost_once = bf16 ? 5 : 2;
+    pl.cost_split = bf16 ? 4 : 2;
+    const int64_t rows = (int64_t)b.n_tokens * c.n_q_heads;
+    pieces = std::min<int64_t>({kPromptMaxPieces, steps, kPagedMaxRows / std::max<int64_t>(rows, 1)});
+    // Whole prompts that fill the GPU are left in one piece (the launch of a merge that has nothing to do is one, too)
+    if (len <= 2 * max_new && pl.blocks * c.n_kv_heads >= pl.places / 2) pieces = 1;
+    pl.n_pieces = (int)std::max<int64_t>(1, pieces);
+    // (one sequence is not made more even by shorter pieces than a place's share, a few by little)
+    pl.shares = std::min<int>(kPromptShares, 1 + b.n_seqs);
+    pl.items = pl.blocks;
+    if (pl.n_pieces > 1)
+      pl.items += std::min((int64_t)pl.shares * pl.places / c.n_kv_heads + pl.shares, pl.blocks * (std::min<int64_t>(pl.n_pieces, ((len + 63) / 64 + pl.shortest - 1) / pl.shortest) - 1));
     pl.rows = pl.n_pieces > 1 ? rows * pl.n_pieces : 0;
+    pl.list = (kPromptHead + (size_t)pl.items * sizeof(PromptItem) + (size_t)pl.blocks * sizeof(int32_t) + 255) / 256 * 256;
   }
   pl.counters = ((size_t)units * kPagedMeetStride * sizeof(uint32_t) + 255) / 256 * 256;  // (always there: steps of either kind share a workspace)
-  pl.bytes = pl.counters + (((size_t)pl.rows * (size_t)(c.head_dim + 2) * sizeof(float)) + 255) / 256 * 256;
+  pl.bytes = pl.counters + pl.list + (((size_t)pl.rows * (size_t)(c.head_dim + 2) * sizeof(float)) + 255) / 256 * 256;
   return pl;
 }
 
