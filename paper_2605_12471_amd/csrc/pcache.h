@@ -88,7 +88,7 @@ struct PromptPlanParams {
   int32_t* head;      // [0] items, [1] blocks to merge, [2] keys of a piece
   PromptItem* items;  // nullptr: no list is asked for
   int32_t* merges;    // behind them: the first pieces of blocks that have several
-  int32_t n_seqs, n_tokens, max_new, max_len, group, unit_rows, max_items, n_pieces, n_kv_heads;
+  int32_t n_seqs, n_tokens, max_new, max_len, group, unit_rows, max_items, max_merges, n_pieces, n_kv_heads;  // (the two bounds hold for sequences that overlap, too)
   int32_t n_places, n_shares, shortest, cost_once, cost_split;  // workgroups that the GPU has room for; of pieces, in tiles; and what one costs, also in tiles
 };
 struct PAppendParams {

@@ -274,6 +274,7 @@ int kvfold_pcache_step(const kvfold_pcache_t* c, int layer, const kvfold_batch_t
     plan.group = p.group;
     plan.unit_rows = pl.unit_rows;
     plan.max_items = (int32_t)pl.items;
+    plan.max_merges = (int32_t)pl.blocks;
     plan.n_pieces = pl.n_pieces;
     plan.n_kv_heads = f.n_kv_heads;
     plan.merges = const_cast<int32_t*>(p.merges);

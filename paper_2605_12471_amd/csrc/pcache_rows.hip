@@ -314,7 +314,7 @@ __device__ void prompt_plan(const PromptPlanParams& p) {
         if (c == kind) to = at[c]++;
       if (write && to < p.max_items) {
         p.items[to] = PromptItem{s0 + lo, t.first, t.n, t.len, b * p.unit_rows, begin, begin + size, pc | n_pieces << 16};
-        if (merge) p.merges[at[kPlanClasses]] = to;
+        if (merge && at[kPlanClasses] < p.max_merges) p.merges[at[kPlanClasses]] = to;
       }
       at[kPlanClasses] += merge;
     }
@@ -347,7 +347,7 @@ __device__ void prompt_plan(const PromptPlanParams& p) {
 #pragma unroll
     for (int c = 0; c < kPlanClasses; ++c) count += total[c];
     p.head[0] = count < p.max_items ? count : p.max_items;
-    p.head[1] = total[kPlanClasses];
+    p.head[1] = total[kPlanClasses] < p.max_merges ? total[kPlanClasses] : p.max_merges;
     p.head[2] = keys;
   }
 }

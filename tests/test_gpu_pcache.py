@@ -20,21 +20,20 @@ class Fold:
     """A batch on a cache whose every row that no sequence has is NaN."""
 
     def __init__(self, hq, hkv, d, page, prev, new, dtype="bf16", seed=0, pad=0, spare=3, layers=1, fused=False, one_each=False, max_new=None, max_len=None, layer=0,
-                 holes=(), present=False):
+                 holes=(), present=False, width=0, lead=0):
         self.hq, self.hkv, self.d, self.page, self.prev, self.new, self.dtype, self.layer = hq, hkv, d, page, list(prev), list(new), dtype, layer
         g = torch.Generator().manual_seed(seed + 977 * sum(prev) + sum(new))
         counts = [-(-(p + n) // page) for p, n in zip(prev, new)]
         self.n_pages = sum(counts) + spare
         self.cache = kv.KvFoldPagedCache(layers, hq, hkv, d, page, self.n_pages, dtype)
         order = torch.randperm(self.n_pages, generator=g).tolist()
-        width = max(counts + [1]) + 2
+        width = max(counts + [1, width - 2]) + 2
         self.tables = torch.full((len(prev), width), -7, dtype=torch.int32)
-        self.rows = self.n_tokens = sum(new) + pad
-        self.n_tokens = sum(new)
+        self.rows, self.n_tokens, self.lead = lead + sum(new) + pad, lead + sum(new), lead
         self.slots = torch.full((self.rows,), -1, dtype=torch.int64)
         shape = (self.n_pages, hkv, page, d)
         self.k_pages, self.v_pages = (torch.full(shape, math.nan, dtype=R.TYPE[dtype]) for _ in range(2))
-        self.k, self.v, at, self.cu = [], [], 0, [0]
+        self.k, self.v, at, self.cu = [], [], lead, [lead]
         if fused:
             together = draw(g, (self.rows, (hq + 2 * hkv) * d), dtype).cuda()
             self.dev = [t.unflatten(1, (-1, d)) for t in together.split((hq * d, hkv * d, hkv * d), 1)]
@@ -96,15 +95,15 @@ class Fold:
                 with np.errstate(invalid="ignore"):
                     bad = np.argwhere(~((np.abs(got - want) <= t) | (got == want)))
                 assert not len(bad), (name, s, self.prev[s], n, len(bad), [(tuple(i), got[tuple(i)], want[tuple(i)], t[tuple(i)]) for i in bad[:4]])
-        assert (out[self.n_tokens:] == 77).all() and (lse[:, self.n_tokens:] == 77).all()
+        assert (out[self.n_tokens:] == 77).all() and (lse[:, self.n_tokens:] == 77).all() and (out[:self.lead] == 77).all() and (lse[:, :self.lead] == 77).all()
         return self
 
     def check_pages(self):
         """The new rows at their places, everything else as it was."""
         for got, want, new in zip(self.cache.view(self.layer), (self.k_pages, self.v_pages), (self.kn, self.vn)):
             want = want.clone()
-            slots = self.slots[:self.n_tokens]
-            want[slots // self.page, :, slots % self.page] = new[:self.n_tokens]
+            slots = self.slots[self.lead:self.n_tokens]
+            want[slots // self.page, :, slots % self.page] = new[self.lead:self.n_tokens]
             view = torch.int16 if self.dtype == "bf16" else torch.int32
             assert torch.equal(got.cpu().view(view), want.view(view))
         return self

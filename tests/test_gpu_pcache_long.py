@@ -1,0 +1,186 @@
+"""The cache in pages where its kernels change with the sizes: long bounds, many sequences, many pages, many pieces, and lengths that are none."""
+import math
+
+import pytest
+import torch
+
+import paper_2605_12471_amd as kv
+import pcache_ref as R
+from test_gpu_pcache import SHAPES, Fold, draw
+
+pytestmark = pytest.mark.gpu
+WIDE = dict(max_len=3000, width=200)  # bounds that long sequences would have
+
+
+@pytest.mark.parametrize("hq,hkv,d", SHAPES + [(28, 4, 128), (32, 8, 64)])
+@pytest.mark.parametrize("page", [16, 64, 256])
+@pytest.mark.parametrize("prev,new", [([0], [257]), ([0, 0, 0], [64, 1, 400]), ([63, 64, 65, 0, 3], [265, 33, 0, 1, 430]), ([0, 500], [300, 40]), ([1000], [133]),
+                                      ([1500, 2300, 7], [131, 140, 129])])
+def test_prompts_under_long_bounds(hq, hkv, d, page, prev, new):
+    Fold(hq, hkv, d, page, prev, new, pad=2, **WIDE).step().check().check_pages()
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (8, 2, 64), (3, 3, 128)])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("prev,new,holes", [
+    ([200, 0, 700], [270, 240, 233], [(0, 0), (0, 2), (1, 0), (2, 1), (2, 10)]), ([5], [250], [(0, 0)]), ([0], [200], [(0, j) for j in range(13)]),
+    ([1000, 300], [129, 140], [(0, j) for j in range(0, 62)] + [(1, j) for j in range(3, 9)])])
+def test_pages_that_are_none_under_long_bounds(hq, hkv, d, prev, new, holes, page):
+    counts = [-(-(p + n) // page) for p, n in zip(prev, new)]
+    Fold(hq, hkv, d, page, prev, new, holes=[(s, j) for s, j in holes if j < counts[s]], **WIDE).step().check()
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (8, 2, 64), (3, 3, 128)])
+@pytest.mark.parametrize("prev,new", [([100, 7, 0], [240, 170, 164]), ([0, 64], [200, 229]), ([1200], [200])])
+def test_no_harm_from_what_rows_do_not_see_under_long_bounds(hq, hkv, d, prev, new):
+    f = Fold(hq, hkv, d, 32, prev, new, seed=5, **WIDE)
+    for s, n in enumerate(new):
+        last = f.cu[s + 1] - 1
+        for t in f.dev[1:]:
+            t[last] = math.nan
+            t[last, 0, :3] = torch.tensor([math.inf, -math.inf, 1.0]).to(t.dtype)
+            t[last - 5, hkv - 1, 7] = math.inf
+            t[last - 70, 0, 9] = -math.inf
+    f.step().check(rows=[n - 71 for n in new])
+
+
+@pytest.mark.parametrize("d,hq", [(64, 4), (128, 2)])
+def test_logits_that_jump_under_long_bounds(d, hq):
+    for gain, shape in ((30.0, lambda j: 1.0 * (j > 500)), (60.0, lambda j: (j % 97 == 0) * 1.0), (0.2, lambda j: j * 1.0), (-90.0, lambda j: 1.0 * (j < 200))):
+        f = Fold(hq, 1, d, 32, [900, 333], [150, 170], seed=2, **WIDE)
+        steer = torch.zeros(d)
+        steer[0] = 8.0
+        for s, n in enumerate(f.new):
+            where, p, at = torch.arange(f.prev[s] + n), f.prev[s], f.cu[s]
+            k = f.k[s].float() * 0.1
+            k[:, 0, 0] = torch.tensor([gain * float(shape(int(j))) for j in where]).clamp(-90, 120)
+            f.k[s] = k.to(torch.bfloat16)
+            f.k_pages[f.tables[s, where[:p] // 32].long(), :, where[:p] % 32] = f.k[s][:p]
+            f.dev[1][at:at + n] = f.k[s][p:].cuda()
+            f.q[at:at + n] = (f.q[at:at + n].float() * 0.1 + steer).to(torch.bfloat16)
+            f.dev[0][at:at + n] = f.q[at:at + n].cuda()
+        f.cache.view(0)[0].copy_(f.k_pages)
+        f.step().check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("prev,new,page", [([9000], [200], 16), ([20000, 5], [40, 33], 16), ([6000, 6100, 100, 0], [64, 70, 200, 300], 32), ([12000], [17], 256)])
+def test_many_pages_and_pieces(dtype, prev, new, page):
+    f = Fold(8, 2, 128, page, prev, new, dtype).step().check().check_pages()
+    out, lse = f.out.clone(), f.lse.clone()
+    for _ in range(2):  # the same bits each time
+        f.step()
+        assert torch.equal(out, f.out) and torch.equal(lse, f.lse)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,d", [(4, 1, 64), (2, 2, 128)])
+@pytest.mark.parametrize("seqs,most", [(257, 40), (300, 1), (700, 23), (1100, 2)])
+def test_many_sequences(seqs, most, hq, hkv, d, dtype):
+    g = torch.Generator().manual_seed(seqs)
+    prev, new = torch.randint(0, 60, (seqs,), generator=g).tolist(), torch.randint(0, most + 1, (seqs,), generator=g).tolist()
+    new[seqs - 1] = most
+    Fold(hq, hkv, d, 16, prev, new, dtype, pad=1).step().check().check_pages()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("prev,new,bound", [([40, 0, 70], [1, 2, 1], None), ([40, 0, 70], [30, 0, 41], None), ([700, 30], [140, 150], 2000)])
+def test_sequences_that_begin_behind_the_first_row(prev, new, bound, dtype):
+    """Rows in front of the first sequence are left as they are, as those behind the last."""
+    Fold(8, 2, 128, 16, prev, new, dtype, lead=5, pad=3, max_len=bound, width=130).step().check().check_pages()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_one_workspace_for_all_kinds_of_steps(dtype):
+    """Prompts, chunks in pieces and decoding of the same sequences, by turns and with the bounds of each."""
+    seqs, hq, hkv, d, page = 3, 8, 2, 128, 32
+    kinds = [dict(prev=[5000, 40, 0], new=[1, 1, 1]), dict(prev=[5000, 64, 0], new=[40, 33, 90]), dict(prev=[0, 0, 0], new=[300, 20, 50]),
+             dict(prev=[9000, 1, 1], new=[2, 1, 0])]
+    folds = [Fold(hq, hkv, d, page, dtype=dtype, seed=i, **kind) for i, kind in enumerate(kinds)]
+    space = max((f.batch.workspace for f in folds), key=lambda t: t.numel())
+    space.zero_()
+    for f in folds:
+        f.batch.workspace = space
+    for turn in range(3):
+        for f in folds if turn % 2 else folds[::-1]:
+            f.step().check().check_pages()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [1, 3, 150])
+def test_lengths_that_are_none(new, dtype):
+    """What lies outside a batch's bounds is taken as the nearest inside: nothing else is read or written."""
+    prev, seqs = [50, 20, 33], 3
+    f = Fold(8, 2, 128, 16, prev, [new] * seqs, dtype, width=30)
+    sound = f.step().check()
+    out, lse = sound.out.clone(), sound.lse.clone()
+    pages = [t.clone() for t in f.cache.view(0)]
+    for lens, cu in (([-5, f.prev[1] + new, 1 << 30], f.cu), ([-2 ** 31, f.prev[1] + new, 2 ** 31 - 1], [-9, f.cu[1], f.cu[2], 2 ** 31 - 1])):
+        f.batch.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        f.batch.cu_new.copy_(torch.tensor(cu, dtype=torch.int32))
+        f.step()
+        torch.cuda.synchronize()
+        mid = slice(f.cu[1], f.cu[2])
+        assert torch.equal(f.out[mid], out[mid]) and torch.equal(f.lse[:, mid], lse[:, mid])
+        assert all(torch.equal(a.nan_to_num(3), b.nan_to_num(3)) for a, b in zip(f.cache.view(0), pages))  # (slots say where the rows go)
+    f.batch.lens.copy_(torch.tensor([p + new for p in prev], dtype=torch.int32))
+    for cu in ([f.cu[3], f.cu[2], f.cu[1], 0], [-1] * 4, [2 ** 31 - 1] * 4):  # nobody has a token
+        f.batch.cu_new.copy_(torch.tensor(cu, dtype=torch.int32))
+        f.step()
+        torch.cuda.synchronize()
+        assert (f.out == 77).all() and (f.lse == 77).all()
+    f.batch.cu_new.copy_(torch.tensor(f.cu, dtype=torch.int32))
+    f.step().check().check_pages()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_prompts_captured_and_replayed(dtype):
+    """assign, a step of prompts beside long sequences and one of decoding in a graph; lengths change between replays, an eager twin gives the same bits."""
+    hq, hkv, d, page, n_pages, seqs, rows = 8, 2, 128, 16, 500, 3, 150
+
+    def state():
+        cache = kv.KvFoldPagedCache(1, hq, hkv, d, page, n_pages, dtype)
+        for t in cache.view(0):
+            t.fill_(0.25)
+        i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+        x = dict(cache=cache, lens=i32([3000, 0, 64]), n_free=i32([n_pages - 192]), free=torch.arange(n_pages, dtype=torch.int32, device="cuda"), new=i32([60, 20, 70]))
+        tables = torch.full((seqs, 260), -1, dtype=torch.int32, device="cuda")
+        tables[0, :188] = torch.arange(n_pages - 188, n_pages)
+        tables[2, :4] = torch.arange(n_pages - 192, n_pages - 188)
+        x["batch"] = kv.KvFoldBatch(cache, tables, rows, 150, 4000)
+        x["q"], x["k"], x["v"] = (torch.zeros((rows, heads, d), dtype=R.TYPE[dtype], device="cuda") for heads in (hq, hkv, hkv))
+        x["out"], x["lse"] = torch.zeros_like(x["q"]), torch.zeros((hq, rows), device="cuda")
+        return x
+
+    def tick(x):
+        x["cache"].assign(x["batch"], x["lens"], x["new"], x["free"], x["n_free"])
+        x["cache"].step(0, x["batch"], x["q"], x["k"], x["v"], x["out"], lse=x["lse"])
+        x["lens"].copy_(x["batch"].lens)
+        x["n_free"].copy_(x["batch"].n_free)
+
+    a, b = state(), state()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        tick(a)
+    torch.cuda.current_stream().wait_stream(side)
+    tick(b)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        tick(a)
+    g = torch.Generator().manual_seed(8)
+    for i, new in enumerate(([1, 100, 30], [0, 0, 150], [2, 2, 2], [150, 0, 0], [50, 50, 50], [0, 0, 0], [0, 149, 1], [33, 1, 60])):
+        fresh = [draw(g, tuple(a[name].shape), dtype) for name in ("q", "k", "v")]
+        for x in (a, b):
+            for name, t in zip(("q", "k", "v"), fresh):
+                x[name].copy_(t)
+            x["new"].copy_(torch.tensor(new, dtype=torch.int32))
+            x["out"].fill_(5)
+            x["lse"].fill_(5)
+        graph.replay()
+        tick(b)
+        if i % 3 == 0:
+            torch.cuda.synchronize()
+        for name in ("out", "lse", "lens", "n_free"):
+            assert torch.equal(a[name], b[name]), (i, name)
+        assert (a["out"][sum(new):] == 5).all() and a["batch"].status.item() == 0
