@@ -865,11 +865,22 @@ class KvFoldPagedCache:
         rc, self.handle = kvfold_pcache_create(self.cfg)
         if rc:
             raise KvFoldError(rc, "kvfold_pcache_create")
-        self._dtype, self._f32, self._i32, self._i64 = torch.float32 if dtype == "f32" else torch.bfloat16, torch.float32, torch.int32, torch.int64
+        self._dtype, self._f32, self._i32, self._i64, self._u8 = torch.float32 if dtype == "f32" else torch.bfloat16, torch.float32, torch.int32, torch.int64, torch.uint8
         self._device, self._hq, self._hkv, self._d, self._page, self._n_pages, self._n_layers = device, n_q_heads, n_kv_heads, head_dim, page_tokens, n_pages, n_layers
         self._lib = load_library()
+        self._bound = False  # as in KvFoldCache
+
+    def _bind(self):
+        native, lib = _native_step(), self._lib
+        if native is None or self.handle is None:
+            self._bound = None
+        else:
+            address = [ctypes.cast(f, ctypes.c_void_p).value for f in (lib.kvfold_pcache_step, lib.kvfold_pcache_assign)]
+            self._bound = native.bind_paged(*address, self.handle.value, self._device, self._hq, self._hkv, self._d, self._n_pages, self.dtype_name != "f32")
+        return self._bound
 
     def close(self):
+        self._bound = None
         if getattr(self, "handle", None) is not None:
             rc = kvfold_pcache_destroy(self.handle)
             self.handle = None
@@ -901,36 +912,64 @@ class KvFoldPagedCache:
     def assign(self, batch, lens, n_new, free_pages, n_free, stream=None):
         """Where the new tokens of the batch's sequences go, into the batch's own tensors (tables, lens, cu_new, slots, positions, n_free, status): lens, n_new int32
         [n_seqs], free_pages int32 [n_pages], n_free int32 [1].  Nothing is synchronised: status says on the device whether there was room."""
+        bound = self._bound
+        if bound is False:
+            bound = self._bind()
+        if bound is not None:
+            rc = _native.paged_assign(bound, lens, n_new, free_pages, n_free, batch.tables, batch.lens, batch.cu_new, batch.slots, batch.positions, batch.n_free,
+                                      batch.status, stream)
+            if rc == 0:
+                return batch
+            if rc is not None:
+                raise KvFoldError(rc, "kvfold_pcache_assign")
         s = batch.n_seqs
+        tables, lens_after, cu_new, slots, positions, n_free_after, status = self._expect_batch(batch)
         rc = self._lib.kvfold_pcache_assign(
             self.handle, s, _expect("lens", lens, self._i32, self._device, (s,)), _expect("n_new", n_new, self._i32, self._device, (s,)),
             _expect("free_pages", free_pages, self._i32, self._device, (self._n_pages,)), _expect("n_free", n_free, self._i32, self._device, (1,)),
-            batch.tables.data_ptr(), batch.tables.shape[1], batch.lens.data_ptr(), batch.cu_new.data_ptr(), batch.slots.data_ptr(), batch.positions.data_ptr(),
-            batch.n_tokens, batch.n_free.data_ptr(), batch.status.data_ptr(), self._stream(stream))
+            tables, batch.tables.shape[1], lens_after, cu_new, slots, positions, batch.n_tokens, n_free_after, status, self._stream(stream))
         if rc:
             raise KvFoldError(rc, "kvfold_pcache_assign")
         return batch
+
+    def _expect_batch(self, batch):
+        """Addresses of the batch's tables, lens, cu_new, slots, positions, n_free and status, which have to be what they were made as."""
+        s, n, i32 = batch.n_seqs, batch.n_tokens, self._i32
+        return [_expect(f"batch.{name}", getattr(batch, name), dtype, self._device, shape) for name, dtype, shape in (
+            ("tables", i32, (s, batch.tables.shape[-1])), ("lens", i32, (s,)), ("cu_new", i32, (s + 1,)), ("slots", self._i64, (n,)), ("positions", i32, (n,)),
+            ("n_free", i32, (1,)), ("status", i32, (1,)))]
 
     def step(self, layer, batch, q, k_new, v_new, out, lse=None, stream=None):
         """Enqueue one fold step of every sequence of the batch: q, out [n_tokens][Hq][d], k_new, v_new [n_tokens][Hkv][d], lse fp32 [Hq][n_tokens].  q, k_new and v_new
         may be parts of one tensor.  k_new = v_new = None: the new rows are in the pages already (``append``)."""
         n = batch.n_tokens
-        desc = batch.desc
+        bound = self._bound
+        if bound is False:
+            bound = self._bind()
+        if bound is not None:
+            rc = _native.paged_step(bound, layer, batch.tables, batch.lens, None if batch.one_each else batch.cu_new, batch.slots, batch.workspace, n, batch.max_new,
+                                    batch.max_len, q, k_new, v_new, out, lse, stream)
+            if rc == 0:
+                return out
+            if rc is not None:
+                raise KvFoldError(rc, "kvfold_pcache_step")
         q_at, q_stride = self._rows("q", q, n, self._hq)
         k_at = v_at = None
-        kv_stride, slots = 0, None
+        kv_stride = 0
         if (k_new is None) != (v_new is None):
             raise ValueError("k_new and v_new: both or neither")
         if k_new is not None:
             (k_at, kv_stride), (v_at, v_stride) = self._rows("k_new", k_new, n, self._hkv), self._rows("v_new", v_new, n, self._hkv)
             if v_stride != kv_stride:
                 raise ValueError(f"v_new: expected the strides of k_new, got {v_new.stride()} beside {k_new.stride()}")
-            slots = batch.slots.data_ptr()
-        step_batch = kvfold_batch_t.from_buffer_copy(desc)
-        step_batch.q_stride, step_batch.kv_stride, step_batch.slots = q_stride, kv_stride, slots
+        tables, lens, cu_new, slots = self._expect_batch(batch)[:4]
+        desc = make_batch(batch.n_seqs, n, batch.max_new, batch.max_len, tables, batch.tables.shape[1], lens, None if batch.one_each else cu_new,
+                          None if k_new is None else slots)
+        desc.q_stride, desc.kv_stride = q_stride, kv_stride
         rc = self._lib.kvfold_pcache_step(
-            self.handle, layer, ctypes.byref(step_batch), q_at, k_at, v_at, _expect("out", out, self._dtype, self._device, (n, self._hq, self._d)),
-            None if lse is None else _expect("lse", lse, self._f32, self._device, (self._hq, n)), batch.workspace.data_ptr(), batch.workspace.numel(), self._stream(stream))
+            self.handle, layer, ctypes.byref(desc), q_at, k_at, v_at, _expect("out", out, self._dtype, self._device, (n, self._hq, self._d)),
+            None if lse is None else _expect("lse", lse, self._f32, self._device, (self._hq, n)),
+            _expect("batch.workspace", batch.workspace, self._u8, self._device, (batch.workspace.numel(),)), batch.workspace.numel(), self._stream(stream))
         if rc:
             raise KvFoldError(rc, "kvfold_pcache_step")
         return out
@@ -982,6 +1021,7 @@ class KvFoldBatch:
         if tables.dim() != 2 or not tables.shape[1]:
             raise ValueError(f"tables: expected [n_seqs][pages], got {tuple(tables.shape)}")
         self.cache, self.tables, self.n_seqs, self.n_tokens, self.one_each = cache, tables, tables.shape[0], n_tokens, one_each
+        self.max_new, self.max_len = max_new, max_len
         where = f"cuda:{dev}"
 
         def mine(name, given, shape, dtype):
@@ -989,15 +1029,13 @@ class KvFoldBatch:
                 return torch.zeros(shape, dtype=dtype, device=where)
             _expect(name, given, dtype, dev, shape)
             return given
-        if n_tokens < 0:
-            raise ValueError(f"n_tokens: expected at least 0, got {n_tokens}")
+        if not (0 <= n_tokens < 1 << 31 and 1 <= max_new < 1 << 31 and 1 <= max_len <= 1 << 30):
+            raise ValueError(f"a batch of {n_tokens} tokens, max_new {max_new}, max_len {max_len} is none")
         self.lens = mine("lens", lens, (self.n_seqs,), torch.int32)
         self.cu_new = mine("cu_new", cu_new, (self.n_seqs + 1,), torch.int32)
         self.slots = mine("slots", slots, (n_tokens,), torch.int64)
         self.positions, self.n_free, self.status = (torch.zeros(shape, dtype=torch.int32, device=where) for shape in ((n_tokens,), (1,), (1,)))
-        self.desc = make_batch(self.n_seqs, n_tokens, max_new, max_len, tables.data_ptr(), tables.shape[1], self.lens.data_ptr(),
-                               None if one_each else self.cu_new.data_ptr(), None)
-        need = kvfold_pcache_workspace_bytes(cache.handle, self.desc)
+        need = kvfold_pcache_workspace_bytes(cache.handle, make_batch(self.n_seqs, n_tokens, max_new, max_len, tables.data_ptr(), tables.shape[1], None, None, None))
         if not need:
             raise ValueError(f"a batch of {self.n_seqs} sequences, {n_tokens} tokens, max_new {max_new}, max_len {max_len} is none")
         self.workspace = torch.zeros((need,), dtype=torch.uint8, device=where)

@@ -6,99 +6,139 @@ namespace kvfold {
 typedef __attribute__((ext_vector_type(4))) unsigned uintx4;
 
 // ---- assign ------------------------------------------------------------------------------------------------------------
-// A few thousand numbers: bound by the chain inside one launch.  Every workgroup goes through all requests for itself, twice: for the totals, which say
-// whether anything is assigned at all, and for the running sums, from which it takes the tokens that are its share of the places (a long prompt's are shared
-// out like any others').  So nobody waits for another workgroup, there is one launch and no memory of its own.  A page is written into its table by the thread
-// whose token is the page's first.
-constexpr int kAssignThreads = 256;
+// A few thousand numbers: bound by the chain inside one launch.  Every workgroup goes through all requests for itself: for the totals, which say whether
+// anything is assigned at all, and for the running sums, from which it takes the tokens that are its share of the places (a long prompt's are shared out like
+// any others').  So nobody waits for another workgroup, there is one launch and no memory of its own.  Up to 1024 requests are gone through once, four a thread, more
+// of them twice.  A page is written into its table by the thread whose token is the page's first.
+constexpr int kAssignThreads = 256, kAssignEach = 4, kAssignChunk = kAssignThreads * kAssignEach;
 
 struct Sums {
   int64_t tokens, pages;
 };
 __device__ __forceinline__ Sums operator+(const Sums& a, const Sums& b) { return Sums{a.tokens + b.tokens, a.pages + b.pages}; }
-__device__ __forceinline__ Sums from_lane(const Sums& a, int lane) { return Sums{(int64_t)__shfl(a.tokens, lane), (int64_t)__shfl(a.pages, lane)}; }
 
-// The sum of the block's values in front of the thread's own; *total: of all.  red: a wavefront's sums.
-__device__ __forceinline__ Sums scan(const Sums& mine, Sums* red, Sums* total) {
+// x and what the lane that CTRL names holds, in the rows (of 16 lanes) of the mask; nothing where there is no such lane
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t plus_lane(int64_t x) {
+  const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, ROWS, 0xf, true);
+  const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)((uint64_t)x >> 32), CTRL, ROWS, 0xf, true);
+  return x + (int64_t)((uint64_t)hi << 32 | lo);
+}
+// The wavefront's running sum, each lane's own value included
+__device__ __forceinline__ int64_t wave_scan(int64_t x) {
+  x = plus_lane<0x111, 0xf>(x);  // lanes 1, 2, 4 and 8 down in the row,
+  x = plus_lane<0x112, 0xf>(x);
+  x = plus_lane<0x114, 0xf>(x);
+  x = plus_lane<0x118, 0xf>(x);
+  x = plus_lane<0x142, 0xa>(x);  // a row's last lane to the next row, of two
+  return plus_lane<0x143, 0xc>(x);  // and lane 31 to the upper half
+}
+
+struct WaveSums {
+  Sums sums;
+  int flags;
+};
+// The sum of the block's values in front of the thread's own; *total, *flags: of all
+__device__ __forceinline__ Sums scan(const Sums& mine, WaveSums* red, Sums* total, int* flags) {
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-  Sums x = mine;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const Sums y = from_lane(x, l < d ? l : l - d);
-    if (l >= d) x = x + y;
-  }
+  const Sums x = {wave_scan(mine.tokens), wave_scan(mine.pages)};
+  const int any = (__any(*flags & 2) ? 2 : 0) | (__any(*flags & 8) ? 8 : 0);
   __syncthreads();  // (red may still be read)
-  if (l == 63) red[w] = x;
+  if (l == 63) red[w] = WaveSums{x, any};
   __syncthreads();
   Sums front = {0, 0}, all = {0, 0};
 #pragma unroll
   for (int i = 0; i < kAssignThreads / 64; ++i) {
-    if (i < w) front = front + red[i];
-    all = all + red[i];
+    const WaveSums y = red[i];
+    if (i < w) front = front + y.sums;
+    all = all + y.sums;
+    *flags |= y.flags;
   }
   *total = all;
   return Sums{front.tokens + x.tokens - mine.tokens, front.pages + x.pages - mine.pages};
 }
 
 __global__ void __launch_bounds__(kAssignThreads) assign_kernel(AssignParams p) {
-  constexpr int NT = kAssignThreads;
-  __shared__ Sums red[NT / 64];
-  __shared__ int wrong;
-  __shared__ int64_t cu[NT + 1], first_page[NT];
-  __shared__ int held[NT], before[NT];  // pages, tokens
+  constexpr int NT = kAssignThreads, EACH = kAssignEach, CHUNK = kAssignChunk;
+  __shared__ WaveSums red[NT / 64];
+  // Of a chunk's requests: what stands in front (below 2^31 where anything is assigned), and the pages and tokens that they hold
+  __shared__ int cu[CHUNK], first_page[CHUNK], held[CHUNK], before[CHUNK];
   const int tid = threadIdx.x, lg = p.page_log2, page = 1 << lg;
   const int64_t t0 = p.n_slots * (int64_t)blockIdx.x / gridDim.x, t1 = p.n_slots * (int64_t)(blockIdx.x + 1) / gridDim.x;
+  const int free_was = *p.n_free;
 
   auto pages_of = [&](int64_t n) -> int64_t { return (n + page - 1) >> lg; };
+  int len[EACH], more[EACH];
+  auto fetch = [&](int s0) {
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int s = s0 + tid * EACH + i;
+      len[i] = s < p.n_seqs ? p.lens[s] : 0;
+      more[i] = s < p.n_seqs ? p.n_new[s] : 0;
+    }
+  };
+  auto needs = [&](int i) -> Sums { return Sums{more[i], pages_of((int64_t)len[i] + more[i]) - pages_of(len[i])}; };
+
   // ---- the totals
-  if (tid == 0) wrong = 0;
-  __syncthreads();
   Sums mine = {0, 0}, total;
   int flags = 0;
-  for (int s = tid; s < p.n_seqs; s += NT) {
-    const int64_t len = p.lens[s], more = p.n_new[s];
-    if (len < 0 || more < 0) {
-      flags |= 8;
-      continue;
+  for (int s0 = 0; s0 < p.n_seqs; s0 += CHUNK) {
+    fetch(s0);
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int64_t after = (int64_t)len[i] + more[i];
+      if (len[i] < 0 || more[i] < 0) {
+        flags |= 8;
+        continue;
+      }
+      if (pages_of(after) > p.table_stride || after > 0x7fffffff) flags |= 2;
+      mine = mine + needs(i);
     }
-    const int64_t after = pages_of(len + more);
-    if (after > p.table_stride || len + more > 0x7fffffff) flags |= 2;
-    mine = mine + Sums{more, after - pages_of(len)};
   }
-  if (flags) atomicOr(&wrong, flags);
-  (void)scan(mine, red, &total);
-  int n_free = *p.n_free;
-  n_free = n_free < 0 ? 0 : n_free > p.n_pages ? p.n_pages : n_free;
-  int status = wrong;
+  Sums front = scan(mine, red, &total, &flags);
+  const int n_free = free_was < 0 ? 0 : free_was > p.n_pages ? p.n_pages : free_was;
+  int status = flags;
   if (total.pages > n_free) status |= 1;
   if (total.tokens > p.n_slots) status |= 4;
   const bool ok = status == 0;
   if (blockIdx.x == 0 && tid == 0) {
     *p.status = status;
-    *p.n_free_after = ok ? n_free - (int)total.pages : *p.n_free;
+    *p.n_free_after = ok ? n_free - (int)total.pages : free_was;
     p.cu_new[0] = 0;
   }
 
-  // ---- the requests in order, NT at a time
-  int64_t tokens = 0, pages = 0;
-  for (int s0 = 0; s0 < p.n_seqs; s0 += NT) {
-    const int s = s0 + tid, n_here = p.n_seqs - s0 < NT ? p.n_seqs - s0 : NT;
-    int64_t len = 0, more = 0;
-    if (s < p.n_seqs) {
-      len = p.lens[s];
-      more = ok ? p.n_new[s] : 0;
+  // ---- the requests in order, a chunk at a time
+  int64_t tokens = 0;
+  int pages = 0;
+  for (int s0 = 0; s0 < p.n_seqs; s0 += CHUNK) {
+    const int n_here = p.n_seqs - s0 < CHUNK ? p.n_seqs - s0 : CHUNK;
+    if (p.n_seqs > CHUNK) {
+      fetch(s0);
+      mine = Sums{0, 0};
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) mine = mine + needs(i);
+      front = scan(mine, red, &total, &flags);  // (whose barriers end the chunk before this one)
     }
-    const Sums own = {more, ok ? pages_of(len + more) - pages_of(len) : 0};
-    const Sums front = scan(own, red, &total);
-    cu[tid] = tokens + front.tokens;
-    first_page[tid] = pages + front.pages;
-    held[tid] = ok ? (int)pages_of(len) : 0;
-    before[tid] = (int)len;
-    if (tid == 0) cu[NT] = tokens + total.tokens;
-    if (blockIdx.x == (unsigned)(s0 / NT) % gridDim.x && s < p.n_seqs) {
-      p.lens_after[s] = (int32_t)(len + more);
-      p.cu_new[s + 1] = (int32_t)(tokens + front.tokens + more);
+    int in_front = ok ? (int)(tokens + front.tokens) : 0, pages_in_front = ok ? pages + (int)front.pages : 0;
+    const bool writes = blockIdx.x == (unsigned)(s0 / CHUNK) % gridDim.x;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int at = tid * EACH + i, s = s0 + at;
+      const Sums own = needs(i);
+      cu[at] = in_front;
+      first_page[at] = pages_in_front;
+      held[at] = (int)pages_of(len[i]);
+      before[at] = len[i];
+      if (ok) {
+        in_front += (int)own.tokens;
+        pages_in_front += (int)own.pages;
+      }
+      if (writes && s < p.n_seqs) {
+        p.lens_after[s] = ok ? len[i] + more[i] : len[i];
+        p.cu_new[s + 1] = in_front;
+      }
     }
+    if (!ok) continue;
     __syncthreads();
     const int64_t from = t0 > tokens ? t0 : tokens, to = t1 < tokens + total.tokens ? t1 : tokens + total.tokens;
     for (int64_t t = from + tid; t < to; t += NT) {
@@ -110,21 +150,16 @@ __global__ void __launch_bounds__(kAssignThreads) assign_kernel(AssignParams p) 
         else
           hi = mid;
       }
-      const int64_t at = before[lo] + (t - cu[lo]), column = at >> lg, lacking = column - held[lo];
+      const int at = before[lo] + ((int)t - cu[lo]), column = at >> lg, lacking = column - held[lo];
       int32_t* row = p.tables + (int64_t)(s0 + lo) * p.table_stride;
-      int32_t number;
-      if (lacking < 0) {
-        number = row[column];
-      } else {
-        number = p.free_pages[n_free - 1 - first_page[lo] - lacking];
-        if ((at & (page - 1)) == 0) row[column] = number;
-      }
+      const int32_t* from_where = lacking < 0 ? row + column : p.free_pages + (n_free - 1 - first_page[lo] - lacking);
+      const int32_t number = *from_where;
+      if (lacking >= 0 && (at & (page - 1)) == 0) row[column] = number;
       p.slots[t] = (int64_t)number * page + (at & (page - 1));
-      if (p.positions) p.positions[t] = (int32_t)at;
+      if (p.positions) p.positions[t] = at;
     }
     tokens += total.tokens;
-    pages += total.pages;
-    __syncthreads();
+    pages += (int)total.pages;
   }
   for (int64_t t = (t0 > tokens ? t0 : tokens) + tid; t < t1; t += NT) {
     p.slots[t] = -1;
@@ -133,8 +168,9 @@ __global__ void __launch_bounds__(kAssignThreads) assign_kernel(AssignParams p) 
 }
 
 hipError_t launch_assign(const AssignParams& p, int n_cu, hipStream_t s) {
-  int64_t wgs = (p.n_slots + 4 * kAssignThreads - 1) / (4 * kAssignThreads);
-  wgs = wgs < 1 ? 1 : wgs > n_cu ? n_cu : wgs;
+  // A token a thread, up to two workgroups a CU: a thread's tokens are looked up one behind the other
+  int64_t wgs = (p.n_slots + kAssignThreads - 1) / kAssignThreads;
+  wgs = wgs < 1 ? 1 : wgs > 2 * n_cu ? 2 * n_cu : wgs;
   hipLaunchKernelGGL(assign_kernel, dim3((unsigned)wgs), dim3(kAssignThreads), 0, s, p);
   return hipGetLastError();
 }

@@ -331,6 +331,129 @@ PyObject* evict(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   }
 }
 
+// ---- the cache in pages -----------------------------------------------------------------------------------------------------
+struct Paged {
+  decltype(&kvfold_pcache_step) step;
+  decltype(&kvfold_pcache_assign) assign;
+  kvfold_pcache_t* handle;
+  int64_t device, n_q_heads, n_kv_heads, head_dim, n_pages;
+  c10::ScalarType dtype;
+};
+
+// bind_paged(step, assign, handle, device, n_q_heads, n_kv_heads, head_dim, n_pages, bf16): the addresses as integers
+PyObject* bind_paged(PyObject*, PyObject* args) {
+  unsigned long long f[2], handle;
+  long long device, hq, hkv, d, pages;
+  int bf16;
+  if (!PyArg_ParseTuple(args, "KKKLLLLLp", &f[0], &f[1], &handle, &device, &hq, &hkv, &d, &pages, &bf16)) return nullptr;
+  return capsule_of(Paged{reinterpret_cast<decltype(&kvfold_pcache_step)>(f[0]), reinterpret_cast<decltype(&kvfold_pcache_assign)>(f[1]),
+                          reinterpret_cast<kvfold_pcache_t*>(handle), device, hq, hkv, d, pages, bf16 ? c10::ScalarType::BFloat16 : c10::ScalarType::Float},
+                    "kvfold_paged");
+}
+
+// Rows [n][heads][d] whose heads lie side by side, and the elements from a token to the next
+void* rows_with_stride(PyObject* obj, const Paged& c, int64_t n, int64_t heads, int64_t* stride) {
+  if (!THPVariable_CheckExact(obj)) return nullptr;
+  const at::Tensor& t = THPVariable_Unpack(obj);
+  const int64_t shape[3] = {n, heads, c.head_dim};
+  if (!t.defined() || !t.has_storage() || t.layout() != c10::kStrided || !t.is_cuda() || t.get_device() != c.device || t.scalar_type() != c.dtype ||
+      t.sizes() != c10::IntArrayRef(shape) || (heads > 1 && t.stride(1) != c.head_dim) || t.stride(2) != 1 || (n > 1 && t.stride(0) < heads * c.head_dim))
+    return nullptr;
+  *stride = n > 1 ? t.stride(0) : heads * c.head_dim;
+  return t.data_ptr();
+}
+
+// Rows and columns of a table of pages, false for anything else
+bool table_of(PyObject* obj, int64_t* rows, int64_t* columns) {
+  if (!THPVariable_CheckExact(obj)) return false;
+  const at::Tensor& t = THPVariable_Unpack(obj);
+  if (!t.defined() || t.dim() != 2 || t.size(0) >= INT32_MAX) return false;
+  *rows = t.size(0);
+  *columns = t.size(1);
+  return true;
+}
+int64_t numel_of(PyObject* obj) { return THPVariable_CheckExact(obj) && THPVariable_Unpack(obj).defined() ? THPVariable_Unpack(obj).numel() : -1; }
+
+// paged_step(cache, layer, tables, lens, cu_new or None, slots, workspace, n_tokens, max_new, max_len, q, k_new, v_new, out, lse, stream)
+PyObject* paged_step(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 16) {
+    PyErr_SetString(PyExc_TypeError, "paged_step: 16 arguments");
+    return nullptr;
+  }
+  const Paged* c = static_cast<Paged*>(PyCapsule_GetPointer(a[0], "kvfold_paged"));
+  if (!c) return nullptr;
+  try {
+    int64_t layer, n, max_new, max_len, seqs, columns, q_stride, kv_stride = 0, v_stride = 0;
+    if (!whole_number(a[1], INT32_MIN, INT32_MAX, &layer) || !whole_number(a[7], 1, INT32_MAX, &n) || !whole_number(a[8], INT32_MIN, INT32_MAX, &max_new) ||
+        !whole_number(a[9], INT64_MIN, INT64_MAX, &max_len) || !table_of(a[2], &seqs, &columns) || seqs < 1)
+      Py_RETURN_NONE;
+    constexpr auto i32 = c10::ScalarType::Int, i64 = c10::ScalarType::Long;
+    const int64_t table[2] = {seqs, columns}, each[1] = {seqs}, sums[1] = {seqs + 1}, tokens[1] = {n}, bytes[1] = {numel_of(a[6])};
+    const int64_t wide[3] = {n, c->n_q_heads, c->head_dim}, per_head[2] = {c->n_q_heads, n};
+    bool ok = true;
+    kvfold_batch_t b;
+    b.struct_size = sizeof b;
+    b.n_seqs = (int32_t)seqs;
+    b.n_tokens = (int32_t)n;
+    b.max_new = (int32_t)max_new;
+    b.max_len = max_len;
+    b.tables = static_cast<int32_t*>(plain(a[2], c->device, i32, table));
+    b.table_stride = columns;
+    b.lens = static_cast<int32_t*>(plain(a[3], c->device, i32, each));
+    b.cu_new = static_cast<int32_t*>(plain_or_none(a[4], c->device, i32, sums, &ok));
+    b.slots = nullptr;
+    void *space = plain(a[6], c->device, c10::ScalarType::Byte, bytes), *q = rows_with_stride(a[10], *c, n, c->n_q_heads, &q_stride), *k = nullptr, *v = nullptr,
+         *out = plain(a[13], c->device, c->dtype, wide), *stream;
+    float* lse = static_cast<float*>(plain_or_none(a[14], c->device, c10::ScalarType::Float, per_head, &ok));
+    if (a[11] != Py_None || a[12] != Py_None) {
+      k = rows_with_stride(a[11], *c, n, c->n_kv_heads, &kv_stride);
+      v = rows_with_stride(a[12], *c, n, c->n_kv_heads, &v_stride);
+      b.slots = static_cast<int64_t*>(plain(a[5], c->device, i64, tokens));
+      ok = ok && k && v && b.slots && kv_stride == v_stride;
+    }
+    if (!ok || !b.tables || !b.lens || !space || !q || !out || !stream_of(a[15], c->device, &stream)) Py_RETURN_NONE;
+    b.q_stride = q_stride;
+    b.kv_stride = kv_stride;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = c->step(c->handle, (int)layer, &b, q, k, v, out, lse, space, (size_t)bytes[0], stream);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(rc);
+  } catch (...) {
+    Py_RETURN_NONE;
+  }
+}
+
+// paged_assign(cache, lens, n_new, free_pages, n_free, tables, lens_after, cu_new, slots, positions, n_free_after, status, stream)
+PyObject* paged_assign(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 13) {
+    PyErr_SetString(PyExc_TypeError, "paged_assign: 13 arguments");
+    return nullptr;
+  }
+  const Paged* c = static_cast<Paged*>(PyCapsule_GetPointer(a[0], "kvfold_paged"));
+  if (!c) return nullptr;
+  try {
+    int64_t seqs, columns;
+    if (!table_of(a[5], &seqs, &columns)) Py_RETURN_NONE;
+    const int64_t table[2] = {seqs, columns}, each[1] = {seqs}, sums[1] = {seqs + 1}, one[1] = {1}, pages[1] = {c->n_pages}, tokens[1] = {numel_of(a[8])};
+    auto i32 = [&](int i, c10::IntArrayRef shape) { return static_cast<int32_t*>(plain(a[i], c->device, c10::ScalarType::Int, shape)); };
+    int32_t *lens = i32(1, each), *n_new = i32(2, each), *free_pages = i32(3, pages), *n_free = i32(4, one), *tables = i32(5, table), *lens_after = i32(6, each),
+            *cu_new = i32(7, sums), *positions = i32(9, tokens), *n_free_after = i32(10, one), *status = i32(11, one);
+    int64_t* slots = static_cast<int64_t*>(plain(a[8], c->device, c10::ScalarType::Long, tokens));
+    void* stream;
+    if (!lens || !n_new || !free_pages || !n_free || !tables || !lens_after || !cu_new || !positions || !n_free_after || !status || !slots ||
+        !stream_of(a[12], c->device, &stream))
+      Py_RETURN_NONE;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = c->assign(c->handle, (int32_t)seqs, lens, n_new, free_pages, n_free, tables, columns, lens_after, cu_new, slots, positions, tokens[0], n_free_after, status, stream);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(rc);
+  } catch (...) {
+    Py_RETURN_NONE;
+  }
+}
+
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyMethodDef fast(const char* name) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F)), METH_FASTCALL, nullptr};
@@ -345,6 +468,9 @@ PyMethodDef methods[] = {
     {"bind_weights", bind_weights, METH_VARARGS, nullptr},
     fast<weigh>("weigh"),
     fast<evict>("evict"),
+    {"bind_paged", bind_paged, METH_VARARGS, nullptr},
+    fast<paged_step>("paged_step"),
+    fast<paged_assign>("paged_assign"),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "kvfold_py_step", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,12 +1,13 @@
 """The cache in pages where its kernels change with the sizes: long bounds, many sequences, many pages, many pieces, and lengths that are none."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
 import paper_2605_12471_amd as kv
 import pcache_ref as R
-from test_gpu_pcache import SHAPES, Fold, draw
+from test_gpu_pcache import SHAPES, Fold, assigned, draw
 
 pytestmark = pytest.mark.gpu
 WIDE = dict(max_len=3000, width=200)  # bounds that long sequences would have
@@ -184,3 +185,40 @@ def test_prompts_captured_and_replayed(dtype):
         for name in ("out", "lse", "lens", "n_free"):
             assert torch.equal(a[name], b[name]), (i, name)
         assert (a["out"][sum(new):] == 5).all() and a["batch"].status.item() == 0
+
+
+# ---- assign: more requests than a workgroup goes through at once, lists that are wrong --------------------------------------------
+@pytest.mark.parametrize("seqs", [1023, 1024, 1025, 2048, 5000])
+@pytest.mark.parametrize("change", [None, "pages", "slots", "negative"])
+def test_assign_for_many_requests(seqs, change):
+    rng = np.random.default_rng(seqs)
+    page, lens, new = 16, rng.integers(0, 70, seqs).tolist(), rng.integers(0, 40, seqs).tolist()
+    up = lambda n: -(-n // page)
+    held, need = [up(p) for p in lens], [up(p + n) - up(p) for p, n in zip(lens, new)]
+    n_pages = sum(held) + sum(need) + 4
+    order = rng.permutation(n_pages).tolist()
+    tables, at = [], 0
+    for h in held:
+        tables.append(order[at:at + h] + [-1] * (8 - h))
+        at += h
+    free = order[at:] + [-1] * at
+    n_free, n_slots = sum(need) - (change == "pages"), sum(new) + 3
+    if change == "slots":
+        n_slots -= 4
+    elif change == "negative":
+        new[seqs - 1] = -1
+    with kv.KvFoldPagedCache(1, 1, 1, 64, page, n_pages) as cache:
+        got = assigned(cache, page, lens, new, free, n_free, tables, n_slots, n_pages)
+    want = R.assign(lens, new, free, n_free, tables, page, n_slots)
+    for name, a, b in zip(("tables", "lens", "cu", "slots", "positions", "n_free", "status"), got, want):
+        assert a == b, name
+
+
+def test_assign_of_numbers_at_the_ends_of_their_types():
+    with kv.KvFoldPagedCache(1, 1, 1, 64, 16, 4) as cache:
+        for lens, new in (([2 ** 31 - 1, 5], [1, 1]), ([0, 0], [2 ** 31 - 1, 2 ** 31 - 1]), ([-2 ** 31, 0], [0, 1]), ([1, 1], [-2 ** 31, 0])):
+            tables, free = [[0, -1], [1, -1]], [2, 3, -1, -1]
+            got = assigned(cache, 16, lens, new, free, 2, tables, 4, 4)
+            want = R.assign(lens, new, free, 2, tables, 16, 4)
+            assert want[-1] and got == list(want)
+        assert assigned(cache, 16, [1], [40], [3, 2, 1, 0], -7, [[0, -1, -1]], 50, 4)[-1] == 1  # no free pages at all
