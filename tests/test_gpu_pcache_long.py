@@ -222,3 +222,29 @@ def test_assign_of_numbers_at_the_ends_of_their_types():
             want = R.assign(lens, new, free, 2, tables, 16, 4)
             assert want[-1] and got == list(want)
         assert assigned(cache, 16, [1], [40], [3, 2, 1, 0], -7, [[0, -1, -1]], 50, 4)[-1] == 1  # no free pages at all
+
+
+# ---- offsets past 32 bits ----------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_pages_far_into_a_large_cache(dtype):
+    """Pages beyond 2^32 bytes of K: the same bits as from a small cache with the same rows."""
+    hq, hkv, d, page = 32, 8, 128, 256
+    n_pages = (5 << 32) // (4 * (2 if dtype == "bf16" else 4) * hkv * page * d)
+    with kv.KvFoldPagedCache(2, hq, hkv, d, page, n_pages, dtype) as large:
+        for prev, new in (([700, 30], [1, 1]), ([700, 30], [3, 2]), ([700, 30], [40, 300]), ([700, 1500], [140, 150]), ([9000], [1])):
+            small = Fold(hq, hkv, d, page, prev, new, dtype).step()
+            out, lse = small.out.clone(), small.lse.clone()
+            far = torch.tensor([n_pages - 1 - 3 * i for i in range(small.n_pages)])
+            f = Fold(hq, hkv, d, page, prev, new, dtype)
+            known = (f.tables >= 0) & (f.tables < f.n_pages)
+            tables = torch.where(known, far[f.tables.clamp(0, f.n_pages - 1).long()].int(), f.tables)
+            slots = torch.where(f.slots >= 0, far[(f.slots // page).clamp(0)] * page + f.slots % page, f.slots)
+            for to, rows in zip(large.view(1), (f.k_pages, f.v_pages)):
+                to[far.cuda()] = rows.cuda()
+            f.batch.tables, f.batch.slots = tables.cuda(), slots.cuda()
+            f.cache, f.layer = large, 1
+            f.step()
+            assert torch.equal(f.out, out) and torch.equal(f.lse, lse)
+            for to, rows in zip(large.view(1), small.cache.view(0)):
+                assert torch.equal(to[far.cuda()].nan_to_num(3), rows.nan_to_num(3))
+            small.check()
