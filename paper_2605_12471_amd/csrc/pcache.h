@@ -23,7 +23,8 @@ struct PagedPlan {
   int units_per_wave;    // prompts: 32-row units of a wavefront
   bool from_end;         // decode: a sequence's last piece is whole, and its first what is left
   int64_t blocks, items;  // prompts: blocks of rows per KV head, and these with a piece of their keys each, at most
-  int places, shares, shortest, cost_once, cost_split;  // PromptPlanParams
+  int places, shortest, step;  // PromptPlanParams
+  float cost_once, cost_piece, cost_merge;
   int n_pieces;          // of the keys, at most
   int piece;             // decode: keys of one, a multiple of 128
   int64_t rows;          // of partial results
@@ -42,8 +43,7 @@ struct PromptItem {
   int32_t piece;               // its number, and how many the block has in all << 16
 };
 static_assert(sizeof(PromptItem) == 32, "an item is fetched at once");
-constexpr int kPromptHead = 64;     // bytes in front of the list: the number of items, of blocks to merge, and the keys of a piece
-constexpr int kPromptShares = 6;    // pieces are no shorter than this part of a place's share of the work
+constexpr int kPromptHead = 64;     // bytes in front of the list: the number of items, and of blocks to merge
 constexpr int kPromptMaxPieces = 64;
 
 // The pieces of `len` keys, one at least
@@ -85,11 +85,13 @@ hipError_t launch_assign(const AssignParams& p, int n_cu, hipStream_t s);
 // The list of a batch's work, made by one workgroup
 struct PromptPlanParams {
   const int32_t *lens, *cu_new;
-  int32_t* head;      // [0] items, [1] blocks to merge, [2] keys of a piece
+  int32_t* head;      // [0] items, [1] blocks to merge
   PromptItem* items;  // nullptr: no list is asked for
   int32_t* merges;    // behind them: the first pieces of blocks that have several
   int32_t n_seqs, n_tokens, max_new, max_len, group, unit_rows, max_items, max_merges, n_pieces, n_kv_heads;  // (the two bounds hold for sequences that overlap, too)
-  int32_t n_places, n_shares, shortest, cost_once, cost_split;  // workgroups that the GPU has room for; of pieces, in tiles; and what one costs, also in tiles
+  int32_t n_places, n_cu;  // workgroups that the GPU has room for; and with a CU each
+  int32_t shortest, step;  // tiles of a piece, at least, and that it is a multiple of
+  float cost_once, cost_piece, cost_merge;  // in tiles: of a workgroup besides its tiles, of a piece besides that, of cutting at all
 };
 struct PAppendParams {
   const void *k, *v;  // [n_tokens][Hkv][d] at token_bytes

@@ -279,10 +279,12 @@ int kvfold_pcache_step(const kvfold_pcache_t* c, int layer, const kvfold_batch_t
     plan.n_kv_heads = f.n_kv_heads;
     plan.merges = const_cast<int32_t*>(p.merges);
     plan.n_places = pl.places;
-    plan.n_shares = pl.shares;
+    plan.n_cu = c->n_cu;
     plan.shortest = pl.shortest;
+    plan.step = pl.step;
     plan.cost_once = pl.cost_once;
-    plan.cost_split = pl.cost_split;
+    plan.cost_piece = pl.cost_piece;
+    plan.cost_merge = pl.cost_merge;
     e = append_rows(c, layer, k_new, v_new, kv_stride, b->slots, fresh ? b->n_tokens : 0, plan, s);
     if (e == hipSuccess) e = launch_attn_prompt(p, f.head_dim, bf16, pl.units_per_wave, s);
     if (e == hipSuccess && pl.n_pieces > 1) e = launch_pmerge(p, f.head_dim, bf16, s);

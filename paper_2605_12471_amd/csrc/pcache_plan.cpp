@@ -62,23 +62,23 @@ PagedPlan make_pplan(const kvfold_pcache_config_t& c, int n_cu, const kvfold_bat
     const bool bf16 = c.dtype == KVFOLD_BF16;
     pl.units_per_wave = bf16 && rows_a_seq > 128 && len > 1024 ? 2 : 1;
     pl.unit_rows = kUnitsPerWg * kRowsPerUnit * pl.units_per_wave;
-    // Blocks of rows: a sequence's last one is filled up.  Pieces: no shorter than a part of a CU's share of all tiles (pcache_rows.hip), so that there are at
-    // most so many more of them.
+    // Blocks of rows: a sequence's last one is filled up.  Pieces: no shorter than a place's share of all tiles (pcache_rows.hip), so that there are at most as many more
+    // as there are places, and those that the device's estimate of the tiles leaves out.
     pl.blocks = (int64_t)b.n_tokens * G / pl.unit_rows + std::min<int64_t>(b.n_seqs, b.n_tokens);
     pl.places = pl.units_per_wave == 2 ? n_cu : 2 * n_cu;
-    pl.shortest = bf16 ? 4 : 2;
-    pl.cost_once = bf16 ? 5 : 2;
-    pl.cost_split = bf16 ? 4 : 2;
+    // (a tile of bf16, two units a wavefront: 1.6 us; of fp32, 64 wide, two workgroups a CU: 7)
+    pl.step = pl.units_per_wave == 2 ? 2 : 1;
+    pl.shortest = bf16 ? 4 : 1;
+    pl.cost_once = bf16 ? 5 : 1;
+    pl.cost_piece = bf16 ? 8 : 0.5f;
+    pl.cost_merge = bf16 ? 8 : 1;
     const int64_t rows = (int64_t)b.n_tokens * c.n_q_heads;
     pieces = std::min<int64_t>({kPromptMaxPieces, steps, kPagedMaxRows / std::max<int64_t>(rows, 1)});
-    // Whole prompts that fill the GPU are left in one piece (the launch of a merge that has nothing to do is one, too)
-    if (len <= 2 * max_new && pl.blocks * c.n_kv_heads >= pl.places / 2) pieces = 1;
+    // Whole prompts that fill the GPU are left in one piece: in bf16 the merge costs more than is won (1000 tokens, 32 heads on 8: 33.8 us, in pieces 38), in fp32 less (147, 114).
+    if (len <= 2 * max_new && pl.blocks * c.n_kv_heads >= (bf16 ? pl.places / 2 : 2 * pl.places)) pieces = 1;
     pl.n_pieces = (int)std::max<int64_t>(1, pieces);
-    // (one sequence is not made more even by shorter pieces than a place's share, a few by little)
-    pl.shares = std::min<int>(kPromptShares, 1 + b.n_seqs);
     pl.items = pl.blocks;
-    if (pl.n_pieces > 1)
-      pl.items += std::min((int64_t)pl.shares * pl.places / c.n_kv_heads + pl.shares, pl.blocks * (std::min<int64_t>(pl.n_pieces, ((len + 63) / 64 + pl.shortest - 1) / pl.shortest) - 1));
+    if (pl.n_pieces > 1) pl.items += std::min<int64_t>(pl.places / c.n_kv_heads + pl.blocks / 8 + 8, pl.blocks * (pl.n_pieces - 1));
     pl.rows = pl.n_pieces > 1 ? rows * pl.n_pieces : 0;
     pl.list = (kPromptHead + (size_t)pl.items * sizeof(PromptItem) + (size_t)pl.blocks * sizeof(int32_t) + 255) / 256 * 256;
   }

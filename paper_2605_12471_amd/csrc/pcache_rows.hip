@@ -177,154 +177,102 @@ hipError_t launch_assign(const AssignParams& p, int n_cu, hipStream_t s) {
 
 // ---- the list of a batch's work ------------------------------------------------------------------------------------------
 // Every sequence's packed rows in blocks, and each block's keys in pieces where that fills the GPU more evenly: it has room for so many workgroups at a time, and
-// sequences differ.  With W tiles in all and N workgroups, pieces of a place's share of them, W / places, or a half ... a sixth of it, are compared with none at
-// all, by the time of (in tiles)
-//   the longest piece and what a workgroup does once, where all are there at the same time; else W and N times what it does once over the places, and half of the
-//   longest for the last round's gaps; and for pieces what they cost besides.
-// The longest come first (five classes).  One workgroup, beside the others that bring the new rows to their places: bound by its chain.  It takes as long as they
-// do for a few hundred tokens.
+// sequences differ.  With W tiles in all, pieces of a place's share of them, W / places, or half as much again, are compared with none at
+// all, by the time of (in tiles at the rate of a full GPU)
+//   the longest piece and what a workgroup does once, where all are there at the same time (less where each has a CU for itself); else W and N times what each of N
+//   does once over the places, and an eighth of the longest for the last round's gaps (of whole blocks: a half); and for pieces what they cost besides.
+// A sequence's blocks are cut at the same keys and stand side by side in the list: they read the same rows at about the same time.  The longest come first (five classes).  One workgroup,
+// beside the others that bring the new rows to their places: bound by its chain.
 constexpr int kPlanThreads = 256;
-constexpr int kPlanClasses = 5, kPlanCounts = kPlanClasses + 1;  // (the last: blocks that are to be merged)
+constexpr int kPlanClasses = 5;
 
-// The block's sums of N values each, for all threads
-template <int N>
-__device__ __forceinline__ void block_sums(int64_t (&x)[N], int64_t (*red)[kPlanThreads / 64]) {
-  const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) x[i] += __shfl_xor(x[i], d);
-  __syncthreads();
-  if (l == 0)
-#pragma unroll
-    for (int i = 0; i < N; ++i) red[i][w] = x[i];
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    x[i] = 0;
-#pragma unroll
-    for (int j = 0; j < kPlanThreads / 64; ++j) x[i] += red[i][j];
-  }
-}
-// The sums of what stands in front of the thread's own values; all[i]: of all
-template <int N>
-__device__ __forceinline__ void block_scan(int (&x)[N], int (&all)[N], int64_t (*red)[kPlanThreads / 64]) {
-  const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int y[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    y[i] = x[i];
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int z = __shfl_up(y[i], d);
-      if (l >= d) y[i] += z;
-    }
-  }
-  __syncthreads();
-  if (l == 63)
-#pragma unroll
-    for (int i = 0; i < N; ++i) red[i][w] = y[i];
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    int before = 0;
-    all[i] = 0;
-#pragma unroll
-    for (int j = 0; j < kPlanThreads / 64; ++j) {
-      const int z = (int)red[i][j];
-      if (j < w) before += z;
-      all[i] += z;
-    }
-    x[i] = before + y[i] - x[i];
-  }
-}
+struct PlanSums {
+  int64_t tiles, blocks;
+  int most;
+};
 
 __device__ void prompt_plan(const PromptPlanParams& p) {
-  constexpr int NT = kPlanThreads;
-  __shared__ int64_t red[kPromptShares > kPlanCounts ? kPromptShares : kPlanCounts][NT / 64];
-  __shared__ int front[NT];  // items in front of a sequence's
-  __shared__ PagedSeq held[NT];
-  const int tid = threadIdx.x;
+  constexpr int NT = kPlanThreads, COUNTS = kPlanClasses + 1;  // (the last: blocks that are to be merged)
+  __shared__ PlanSums red[NT / 64];
+  __shared__ int front[NT];  // of a chunk's sequences: the blocks in front of theirs,
+  __shared__ PagedSeq held[NT];  // and themselves
+  __shared__ int counts[2][COUNTS];
+  const int tid = threadIdx.x, l = tid & 63, w = tid >> 6;
   const bool once = p.n_seqs <= NT;  // each thread has one sequence, for good
-  auto fetch = [&](int s) -> PagedSeq {
-    if (s >= p.n_seqs) return PagedSeq{0, 0, 0};
-    return paged_seq(p.cu_new ? p.cu_new[s] : s, p.cu_new ? p.cu_new[s + 1] : s + 1, p.lens[s], p.n_tokens, p.max_new, p.max_len);
-  };
-  const PagedSeq own = fetch(tid);
-  auto seq_at = [&](int s0) -> PagedSeq { return s0 ? fetch(s0 + tid) : own; };
+  if (tid < 2 * COUNTS) counts[0][tid] = 0;
   auto blocks_of = [&](const PagedSeq& q) -> int { return (int)((unsigned)(q.n * p.group + p.unit_rows - 1) / (unsigned)p.unit_rows); };
-  auto tiles_of = [&](const PagedSeq& q) -> int { return (q.len + 63) / 64; };
-
-  // ---- the pieces' length, in tiles
-  int64_t sums[2] = {0, 0};  // tiles, blocks
-  int most = 2;
-  for (int s0 = 0; s0 < p.n_seqs; s0 += NT) {
-    const PagedSeq q = seq_at(s0);
-    const int nb = blocks_of(q), keys = q.len - q.n / 2;
-    sums[0] += (int64_t)nb * ((keys > 0 ? keys : 0) / 64 + 1);
-    sums[1] += nb;
-    if (nb && tiles_of(q) > most) most = tiles_of(q);
-  }
+  // A chunk's sequences into LDS, with what stands in front of them in the chunk; returns the chunk's sums
+  auto chunk = [&](int s0) -> PlanSums {
+    const int s = s0 + tid;
+    PagedSeq q = {0, 0, 0};
+    if (s < p.n_seqs) q = paged_seq(p.cu_new ? p.cu_new[s] : s, p.cu_new ? p.cu_new[s + 1] : s + 1, p.lens[s], p.n_tokens, p.max_new, p.max_len);
+    const int nb = blocks_of(q);
+    const int keys = q.len - q.n / 2;  // of a block, about
+    const int64_t tiles = wave_scan((int64_t)nb * ((keys > 0 ? keys : 0) / 64 + 1)), blocks = wave_scan((int64_t)nb);
+    int most = nb ? (q.len + 63) / 64 : 0;
 #pragma unroll
-  for (int d = 32; d > 0; d /= 2) {
-    const int y = __shfl_xor(most, d);
-    most = y > most ? y : most;
-  }
-  if ((tid & 63) == 0) front[tid >> 6] = most;
-  block_sums(sums, red);
-#pragma unroll
-  for (int i = 0; i < NT / 64; ++i) most = front[i] > most ? front[i] : most;
-  most = (most + 1) / 2 * 2;  // (pieces are whole steps of 128 keys)
-  const int64_t work = sums[0] * p.n_kv_heads;
-  int piece = most;
-  if (p.n_pieces > 1) {
-    int len[kPromptShares];
-    int64_t n[kPromptShares];
-    const int64_t share = (work + p.n_places - 1) / p.n_places;
-    const int least = (most + p.n_pieces - 1) / p.n_pieces;
-#pragma unroll
-    for (int k = 0; k < kPromptShares; ++k) {
-      int64_t x = (share + k) / (k + 1);
-      x = x < least ? least : x;
-      x = x < p.shortest ? p.shortest : x;
-      len[k] = x < most ? ((int)x + 1) / 2 * 2 : most;
-      n[k] = 0;
+    for (int d = 32; d > 0; d /= 2) {
+      const int y = __shfl_xor(most, d);
+      most = y > most ? y : most;
     }
-    for (int s0 = 0; s0 < p.n_seqs; s0 += NT) {
-      const PagedSeq q = seq_at(s0);
-      const int nb = blocks_of(q), tiles = tiles_of(q);
+    __syncthreads();  // (what is read of LDS is read)
+    if (l == 63) red[w] = PlanSums{tiles, blocks, most};
+    __syncthreads();
+    int64_t before = 0;
+    PlanSums all = {0, 0, 0};
 #pragma unroll
-      for (int k = 0; k < kPromptShares; ++k) n[k] += (int64_t)nb * (int)((unsigned)(tiles + len[k] - 1) / (unsigned)len[k]);
+    for (int i = 0; i < NT / 64; ++i) {
+      const PlanSums y = red[i];
+      if (i < w) before += y.blocks;
+      all.tiles += y.tiles;
+      all.blocks += y.blocks;
+      all.most = y.most > all.most ? y.most : all.most;
     }
-    block_sums(n, red);
-    auto cost = [&](int longest, int64_t wgs, int each) -> int64_t {
-      return wgs <= p.n_places ? longest + each : (work + wgs * each) / p.n_places + (longest + each) / 2;
-    };
-    int64_t best = cost(most, sums[1] * p.n_kv_heads, p.cost_once);
-#pragma unroll
-    for (int k = 0; k < kPromptShares; ++k) {
-      const int64_t wgs = n[k] * p.n_kv_heads, t = cost(len[k], wgs, p.cost_once + p.cost_split) + p.cost_split;
-      if (k < p.n_shares && len[k] < most && t < best && n[k] <= p.max_items) {
-        best = t;
-        piece = len[k];
-      }
-    }
-  }
-  const int keys = piece * 64;
-
-  // ---- the items: counted by classes, then written, each thread's behind those of the threads before it
-  int at[kPlanCounts] = {}, total[kPlanCounts] = {};
-  auto walk = [&](int s0, bool write) {
-    const PagedSeq q = seq_at(s0);
-    int x[1] = {blocks_of(q) * paged_pieces(q.len, keys)}, all[1];  // every block's pieces, of the sequence's last row (those that a block does not see are passed over)
-    __syncthreads();  // (what is read of front and held is read)
-    block_scan(x, all, red);
-    front[tid] = x[0];
+    front[tid] = (int)(before + blocks) - nb;
     held[tid] = q;
     __syncthreads();
-    const int n_here = p.n_seqs - s0 < NT ? p.n_seqs - s0 : NT;
-    for (int i = tid; i < all[0]; i += NT) {
-      int lo = 0, hi = n_here;
+    return all;
+  };
+
+  // ---- all of the work, and whether it is cut
+  PlanSums all = chunk(0);
+  for (int s0 = NT; s0 < p.n_seqs; s0 += NT) {
+    const PlanSums y = chunk(s0);
+    all.tiles += y.tiles;
+    all.blocks += y.blocks;
+    all.most = y.most > all.most ? y.most : all.most;
+  }
+  if (all.blocks > p.max_merges) {  // sequences that overlap: no work at all, rather than more than there can be
+    if (tid < 2) p.head[tid] = 0;
+    return;
+  }
+  const int most = all.most > 1 ? all.most : 1;
+  int piece = most;
+  if (p.n_pieces > 1) {
+    const float work = (float)(all.tiles * p.n_kv_heads), places = (float)p.n_places, alone = (float)p.n_cu;
+    auto cost = [&](float longest, float wgs, float each, float gaps) -> float {
+      return wgs <= alone ? longest * alone / places + each : wgs <= places ? longest + each : (work + wgs * each) / places + (longest + each) * gaps;
+    };
+    const float whole = cost((float)most, (float)(all.blocks * p.n_kv_heads), p.cost_once, 0.5f);
+    // in the lanes: a place's share, and half as much again
+    const int j = 2 + (l & 1), least = (most + p.n_pieces - 1) / p.n_pieces;
+    int len = (int)fminf(ceilf(work * (float)j / (2.f * places)), 1e9f);
+    len = len < least ? least : len;
+    len = len < p.shortest ? p.shortest : len;
+    len = (len + p.step - 1) / p.step * p.step;
+    const float wgs = ((float)all.tiles / (float)len + 0.5f * (float)all.blocks) * (float)p.n_kv_heads;
+    float t = cost((float)len, wgs, p.cost_once + p.cost_piece, 0.125f) + p.cost_merge;
+    if (len >= most) t = INFINITY;
+    const float t2 = __shfl_xor(t, 1);
+    const int len2 = __shfl_xor(len, 1);
+    if (t2 < t || (t2 == t && len2 > len)) t = t2, len = len2;
+    if (t < whole) piece = len;
+  }
+
+  // ---- the items: counted by classes, then written
+  auto items = [&](int n_here, int s0, bool write) {
+    for (int i = tid; i < n_here; i += NT) {
+      int lo = 0, hi = p.n_seqs - s0 < NT ? p.n_seqs - s0 : NT;
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (front[mid] <= i)
@@ -333,58 +281,57 @@ __device__ void prompt_plan(const PromptPlanParams& p) {
           hi = mid;
       }
       const PagedSeq t = held[lo];
-      const int nb = blocks_of(t), n_of = paged_pieces(t.len, keys), j = i - front[lo];
-      const int back = (int)((unsigned)j / (unsigned)nb), pc = n_of - 1 - back, b = nb - 1 - (j - back * nb);  // (the blocks of a piece side by side)
+      const int b = i - front[lo];
       int last = (b + 1) * p.unit_rows;  // (below 2^29)
       last = last < t.n * p.group ? last : t.n * p.group;
       int seen = t.len - t.n + (int)((unsigned)(last - 1) / (unsigned)p.group) + 1;  // keys that the block's last row sees
       seen = seen < 0 ? 0 : seen;
-      const int n_pieces = paged_pieces(seen, keys);
-      if (pc >= n_pieces) continue;
-      const int begin = pc * keys, end = begin + keys < seen ? begin + keys : seen, size = end > begin ? end - begin : 0;
-      const int kind = size >= keys ? 0 : kPlanClasses - 1 - (int)((unsigned)((size >> 6) * 4) / (unsigned)piece);
-      const bool merge = n_pieces > 1 && pc == 0;
-      int to = 0;
-#pragma unroll
-      for (int c = 0; c < kPlanClasses; ++c)
-        if (c == kind) to = at[c]++;
-      if (write && to < p.max_items) {
-        p.items[to] = PromptItem{s0 + lo, t.first, t.n, t.len, b * p.unit_rows, begin, begin + size, pc | n_pieces << 16};
-        if (merge && at[kPlanClasses] < p.max_merges) p.merges[at[kPlanClasses]] = to;
+      const int n = paged_pieces(seen, piece * 64);
+      for (int pc = 0; pc < n; ++pc) {
+        const int from = pc * piece * 64, to = pc + 1 < n ? from + piece * 64 : seen, size = (to - from) >> 6;
+        const int kind = size >= piece ? 0 : kPlanClasses - 1 - (int)((unsigned)(size * 4) / (unsigned)piece);
+        const unsigned slot = (unsigned)atomicAdd(&counts[write][kind], 1);
+        if (!write || slot >= (unsigned)p.max_items) continue;
+        p.items[slot] = PromptItem{s0 + lo, t.first, t.n, t.len, b * p.unit_rows, from, to, pc | n << 16};
+        if (n > 1 && pc == 0) {
+          const unsigned at = (unsigned)atomicAdd(&counts[1][kPlanClasses], 1);
+          if (at < (unsigned)p.max_merges) p.merges[at] = (int)slot;
+        }
       }
-      at[kPlanClasses] += merge;
     }
   };
-  if (!once) {  // (all chunks' counts, for where the classes begin)
-    for (int s0 = 0; s0 < p.n_seqs; s0 += NT) walk(s0, false);
-    block_scan(at, total, red);
-  }
-  int base[kPlanCounts] = {};
-  for (int s0 = 0; s0 < p.n_seqs; s0 += NT) {
-    int here[kPlanCounts];
-#pragma unroll
-    for (int c = 0; c < kPlanCounts; ++c) at[c] = 0;
-    walk(s0, false);
-    block_scan(at, here, red);
-    if (once)
-#pragma unroll
-      for (int c = 0; c < kPlanCounts; ++c) total[c] = here[c];
-    int begin = 0;
-#pragma unroll
-    for (int c = 0; c < kPlanCounts; ++c) {
-      at[c] += base[c] + (c < kPlanClasses ? begin : 0);
-      begin += total[c];
-      base[c] += here[c];
+  int total = 0;
+  for (;;) {
+    for (int s0 = 0; s0 < p.n_seqs; s0 += NT) {
+      PlanSums y = all;
+      if (!once) y = chunk(s0);
+      items((int)y.blocks, s0, false);
     }
-    walk(s0, true);
-  }
-  if (tid == 0) {
-    int count = 0;
+    __syncthreads();
+    total = 0;
 #pragma unroll
-    for (int c = 0; c < kPlanClasses; ++c) count += total[c];
-    p.head[0] = count < p.max_items ? count : p.max_items;
-    p.head[1] = total[kPlanClasses] < p.max_merges ? total[kPlanClasses] : p.max_merges;
-    p.head[2] = keys;
+    for (int c = 0; c < kPlanClasses; ++c) total += counts[0][c];
+    if (piece == most || total <= p.max_items) break;
+    piece = most;  // more than the list has room for
+    __syncthreads();
+    if (tid < COUNTS) counts[0][tid] = 0;
+    __syncthreads();
+  }
+  if (tid < kPlanClasses) {
+    int begin = 0;
+    for (int c = 0; c < tid; ++c) begin += counts[0][c];
+    counts[1][tid] = begin;
+  }
+  __syncthreads();
+  for (int s0 = 0; s0 < p.n_seqs; s0 += NT) {
+    PlanSums y = all;
+    if (!once) y = chunk(s0);
+    items((int)y.blocks, s0, true);
+  }
+  __syncthreads();
+  if (tid == 0) {
+    p.head[0] = total < p.max_items ? total : p.max_items;
+    p.head[1] = counts[1][kPlanClasses] < p.max_merges ? counts[1][kPlanClasses] : p.max_merges;
   }
 }
 

@@ -125,6 +125,9 @@ def test_lengths_that_are_none(new, dtype):
         assert torch.equal(f.out[mid], out[mid]) and torch.equal(f.lse[:, mid], lse[:, mid])
         assert all(torch.equal(a.nan_to_num(3), b.nan_to_num(3)) for a, b in zip(f.cache.view(0), pages))  # (slots say where the rows go)
     f.batch.lens.copy_(torch.tensor([p + new for p in prev], dtype=torch.int32))
+    f.batch.cu_new.copy_(torch.tensor([0, 3 * new, 0, 3 * new], dtype=torch.int32))  # two that overlap: ends, whatever the results are
+    f.step()
+    torch.cuda.synchronize()
     for cu in ([f.cu[3], f.cu[2], f.cu[1], 0], [-1] * 4, [2 ** 31 - 1] * 4):  # nobody has a token
         f.batch.cu_new.copy_(torch.tensor(cu, dtype=torch.int32))
         f.step()
