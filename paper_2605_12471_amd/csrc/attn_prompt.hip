@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(256, 1) attn_prompt_kernel(PAttnParams p) {
   // ---- the first tile with keys of a page that is none: each wavefront looks through the piece's part of the table, 64 pages at a time
   int t_bad = 0x7fffffff;
   if (t_begin < t_end) {
-    const int last = (wk.key_end - 1) >> p.page_log2;
+    const int last = ((t_end * BN < len ? t_end * BN : len) - 1) >> p.page_log2;  // (tiles are brought whole, also the piece's last one)
 #pragma unroll 1
     for (int i = wk.key_begin >> p.page_log2; i <= last; i += 64) {
       const int32_t number = i + l <= last ? p.tables[(int64_t)wk.seq * p.table_stride + i + l] : 0;

@@ -31,6 +31,15 @@ def test_pages_that_are_none_under_long_bounds(hq, hkv, d, prev, new, holes, pag
     Fold(hq, hkv, d, page, prev, new, holes=[(s, j) for s, j in holes if j < counts[s]], **WIDE).step().check()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (8, 2, 64), (2, 2, 128)])
+@pytest.mark.parametrize("bound", [None, 3000])
+def test_one_page_that_is_none(bound, hq, hkv, d, dtype):
+    """Each in turn, also behind the last key that a block of rows sees, inside its last tile."""
+    for j in range(2, 19):
+        Fold(hq, hkv, d, 16, [40, 7], [260, 300], dtype, holes=[(0, j), (1, j)], max_len=bound, width=200).step().check()
+
+
 @pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (8, 2, 64), (3, 3, 128)])
 @pytest.mark.parametrize("prev,new", [([100, 7, 0], [240, 170, 164]), ([0, 64], [200, 229]), ([1200], [200])])
 def test_no_harm_from_what_rows_do_not_see_under_long_bounds(hq, hkv, d, prev, new):
