@@ -1267,31 +1267,29 @@ hipError_t launch_attn_prompt(const PAttnParams& p, int head_dim, bool bf16, int
 }
 
 // ---- the merge of pieces ---------------------------------------------------------------------------------------------------
-// A thread has 16 bytes of a row and goes through its pieces, eight in flight; rows of one piece have been written.  Bound by memory.
-constexpr int kMergeRows = 32;  // of a workgroup
+// A thread has 16 bytes of a row and goes through its pieces, eight in flight; rows of one piece have been written.  Bound by memory, and by the way to the first bytes: a
+// workgroup has no second rows, which would wait for its first (chunks of 45 tokens of 8 sequences in 16 pieces: 8.5 us, with four rows a thread 17.4; of 256 tokens of
+// 28 heads on 4: 13.2 and 21.1, which is 3.4 TB/s of partial results).
 template <class T, int D>
 __global__ void __launch_bounds__(256) pmerge_kernel(PAttnParams p, int parts_log2) {
-  constexpr int V = D / 4, ROWS = 256 / V;  // (unit_rows / kMergeRows = 2^parts_log2 workgroups share a block's rows)
+  constexpr int V = D / 4, ROWS = 256 / V, N = 8;  // (unit_rows / ROWS = 2^parts_log2 workgroups share a block's rows)
   const unsigned id = blockIdx.x >> parts_log2;
   const int at_block = (int)quot(id, p.by_kv_heads);
   if (at_block >= ((ConstPtr<int32_t>)(uintptr_t)p.list_head)[1]) return;
   const PromptWork wk = prompt_item(p, ((ConstPtr<int32_t>)(uintptr_t)p.merges)[at_block], (int)id - at_block * p.n_kv_heads);
-  const int n = wk.n_pieces;
-  const int c = threadIdx.x % V, first = wk.row0 + (int)(blockIdx.x & ((1u << parts_log2) - 1)) * kMergeRows;
-#pragma unroll 1
-  for (int r = first + threadIdx.x / V; r < first + kMergeRows && r < wk.rows; r += ROWS) {
-  const int tok = (int)quot((unsigned)r, p.by_group), head = wk.g * p.group + r - tok * p.group;
-  const int64_t n_rows = (int64_t)p.n_tokens * p.n_q_heads, token = wk.sq.first + tok, at = token * p.n_q_heads + head;
+  const int n = wk.n_pieces, c = threadIdx.x % V, r = wk.row0 + (int)(blockIdx.x & ((1u << parts_log2) - 1)) * ROWS + (int)threadIdx.x / V;
+  if (r >= wk.rows) return;
+  const unsigned place = prompt_place(p, wk, r), Hq = (unsigned)p.n_q_heads;
+  const int64_t n_rows = (int64_t)p.n_tokens * Hq;
   float M = -INFINITY, L = 0.f;
   floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-  constexpr int N = 8;
 #pragma unroll 1
   for (int i0 = 0; i0 < n; i0 += N) {
     floatx2 ml[N];
     floatx4 o[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int64_t part = (int64_t)(i0 + i < n ? i0 + i : n - 1) * n_rows + at;
+      const int64_t part = (int64_t)(i0 + i < n ? i0 + i : n - 1) * n_rows + place;
       ml[i] = *reinterpret_cast<const floatx2*>(p.part_ml + part * 2);
       o[i] = *reinterpret_cast<const floatx4*>(p.part_o + part * D + c * 4);
     }
@@ -1320,21 +1318,23 @@ __global__ void __launch_bounds__(256) pmerge_kernel(PAttnParams p, int parts_lo
   const float inv = 1.f / L;
 #pragma unroll
   for (int e = 0; e < 4; ++e) acc[e] = L == 0.f ? 0.f : acc[e] * inv;
+  const uint64_t at = (uint64_t)place * D + (unsigned)c * 4u;
   if constexpr (sizeof(T) == 2) {
     bf16x4 v;
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = (__bf16)acc[e];
-    *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p.out) + at * D + c * 4) = v;
+    *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p.out) + at) = v;
   } else {
-    *reinterpret_cast<floatx4*>(static_cast<float*>(p.out) + at * D + c * 4) = acc;
+    *reinterpret_cast<floatx4*>(static_cast<float*>(p.out) + at) = acc;
   }
-  if (p.lse && c == 0) p.lse[(int64_t)head * p.n_tokens + token] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * 0.6931471805599453f;
-  }
+  const unsigned token = place / Hq;
+  if (p.lse && c == 0) p.lse[(int64_t)(place - token * Hq) * p.n_tokens + token] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * 0.6931471805599453f;
 }
 
 hipError_t launch_pmerge(const PAttnParams& p, int head_dim, bool bf16, hipStream_t s) {
+  const int rows = 256 / (head_dim / 4);
   int lg = 0;
-  while (kMergeRows << lg < p.unit_rows) ++lg;
+  while (rows << lg < p.unit_rows) ++lg;
   const dim3 grid(((unsigned)p.n_blocks * (unsigned)p.n_kv_heads) << lg), block(256);
   if (bf16 && head_dim == 128)
     hipLaunchKernelGGL((pmerge_kernel<__bf16, 128>), grid, block, 0, s, p, lg);

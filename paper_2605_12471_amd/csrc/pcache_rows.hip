@@ -271,32 +271,33 @@ __device__ void prompt_plan(const PromptPlanParams& p) {
 
   // ---- the items: counted by classes, then written
   auto items = [&](int n_here, int s0, bool write) {
-    for (int i = tid; i < n_here; i += NT) {
+    const int n_most = (most + piece - 1) / piece;
+    for (int i = tid; i < n_here * n_most; i += NT) {  // (below 2^28; the blocks of a piece side by side)
+      const int pc = (int)((unsigned)i / (unsigned)n_here), block = i - pc * n_here;
       int lo = 0, hi = p.n_seqs - s0 < NT ? p.n_seqs - s0 : NT;
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (front[mid] <= i)
+        if (front[mid] <= block)
           lo = mid;
         else
           hi = mid;
       }
       const PagedSeq t = held[lo];
-      const int b = i - front[lo];
+      const int b = block - front[lo];
       int last = (b + 1) * p.unit_rows;  // (below 2^29)
       last = last < t.n * p.group ? last : t.n * p.group;
       int seen = t.len - t.n + (int)((unsigned)(last - 1) / (unsigned)p.group) + 1;  // keys that the block's last row sees
       seen = seen < 0 ? 0 : seen;
       const int n = paged_pieces(seen, piece * 64);
-      for (int pc = 0; pc < n; ++pc) {
-        const int from = pc * piece * 64, to = pc + 1 < n ? from + piece * 64 : seen, size = (to - from) >> 6;
-        const int kind = size >= piece ? 0 : kPlanClasses - 1 - (int)((unsigned)(size * 4) / (unsigned)piece);
-        const unsigned slot = (unsigned)atomicAdd(&counts[write][kind], 1);
-        if (!write || slot >= (unsigned)p.max_items) continue;
-        p.items[slot] = PromptItem{s0 + lo, t.first, t.n, t.len, b * p.unit_rows, from, to, pc | n << 16};
-        if (n > 1 && pc == 0) {
-          const unsigned at = (unsigned)atomicAdd(&counts[1][kPlanClasses], 1);
-          if (at < (unsigned)p.max_merges) p.merges[at] = (int)slot;
-        }
+      if (pc >= n) continue;
+      const int from = pc * piece * 64, to = pc + 1 < n ? from + piece * 64 : seen, size = (to - from) >> 6;
+      const int kind = size >= piece ? 0 : kPlanClasses - 1 - (int)((unsigned)(size * 4) / (unsigned)piece);
+      const unsigned slot = (unsigned)atomicAdd(&counts[write][kind], 1);
+      if (!write || slot >= (unsigned)p.max_items) continue;
+      p.items[slot] = PromptItem{s0 + lo, t.first, t.n, t.len, b * p.unit_rows, from, to, pc | n << 16};
+      if (n > 1 && pc == 0) {
+        const unsigned at = (unsigned)atomicAdd(&counts[1][kPlanClasses], 1);
+        if (at < (unsigned)p.max_merges) p.merges[at] = (int)slot;
       }
     }
   };
