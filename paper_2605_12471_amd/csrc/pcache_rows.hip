@@ -177,7 +177,7 @@ hipError_t launch_assign(const AssignParams& p, int n_cu, hipStream_t s) {
 
 // ---- the list of a batch's work ------------------------------------------------------------------------------------------
 // Every sequence's packed rows in blocks, and each block's keys in pieces where that fills the GPU more evenly: it has room for so many workgroups at a time, and
-// sequences differ.  With W tiles in all, pieces of a place's share of them, W / places, or half as much again, are compared with none at
+// sequences differ.  With W tiles in all, pieces of a place's share of them, W / places, or an eighth to three more, are compared with none at
 // all, by the time of (in tiles at the rate of a full GPU)
 //   the longest piece and what a workgroup does once, where all are there at the same time (less where each has a CU for itself); else W and N times what each of N
 //   does once over the places, and an eighth of the longest for the last round's gaps (of whole blocks: a half); and for pieces what they cost besides.
@@ -185,6 +185,7 @@ hipError_t launch_assign(const AssignParams& p, int n_cu, hipStream_t s) {
 // beside the others that bring the new rows to their places: bound by its chain.
 constexpr int kPlanThreads = 256;
 constexpr int kPlanClasses = 5;
+constexpr int kPlanLengths = 4;  // of a piece that are looked at, an eighth of a share apart
 
 struct PlanSums {
   int64_t tiles, blocks;
@@ -197,6 +198,7 @@ __device__ void prompt_plan(const PromptPlanParams& p) {
   __shared__ int front[NT];  // of a chunk's sequences: the blocks in front of theirs,
   __shared__ PagedSeq held[NT];  // and themselves
   __shared__ int counts[2][COUNTS];
+  __shared__ int64_t lengths[kPlanLengths][NT / 64];
   const int tid = threadIdx.x, l = tid & 63, w = tid >> 6;
   const bool once = p.n_seqs <= NT;  // each thread has one sequence, for good
   if (tid < 2 * COUNTS) counts[0][tid] = 0;
@@ -253,20 +255,51 @@ __device__ void prompt_plan(const PromptPlanParams& p) {
     auto cost = [&](float longest, float wgs, float each, float gaps) -> float {
       return wgs <= alone ? longest * alone / places + each : wgs <= places ? longest + each : (work + wgs * each) / places + (longest + each) * gaps;
     };
+    const int least = (most + p.n_pieces - 1) / p.n_pieces;
+    int len[kPlanLengths];
+    int64_t pieces[kPlanLengths];
+#pragma unroll
+    for (int k = 0; k < kPlanLengths; ++k) {
+      int x = (int)fminf(ceilf(work * (1.f + 0.125f * (float)k) / places), 1e9f);
+      x = x < least ? least : x;
+      x = x < p.shortest ? p.shortest : x;
+      len[k] = (x + p.step - 1) / p.step * p.step;
+      pieces[k] = 0;
+    }
+    for (int s0 = 0; s0 < p.n_seqs; s0 += NT) {
+      if (!once) (void)chunk(s0);
+      const PagedSeq q = held[tid];
+      const int nb = blocks_of(q), sees = (q.len > q.n ? q.len - q.n : 0) + p.unit_rows / p.group, first = ((sees < q.len ? sees : q.len) + 63) / 64, last = (q.len + 63) / 64;
+#pragma unroll
+      for (int k = 0; k < kPlanLengths; ++k)  // (of the first block and the last, halved below)
+        pieces[k] += (int64_t)nb * ((int)((unsigned)(first + len[k] - 1) / (unsigned)len[k]) + (int)((unsigned)(last + len[k] - 1) / (unsigned)len[k]));
+    }
+    // (each length's sum in a lane of its own from here on)
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kPlanLengths; ++k) {
+      const int64_t sum = wave_scan(pieces[k]);
+      if (l == 63) lengths[k][w] = sum;
+    }
+    __syncthreads();
+    const int k0 = l & (kPlanLengths - 1);
+    int64_t wgs = 0;
+#pragma unroll
+    for (int i = 0; i < NT / 64; ++i) wgs += lengths[k0][i];
+    wgs = (wgs + 1) / 2;
+    int best = len[0];
+#pragma unroll
+    for (int k = 1; k < kPlanLengths; ++k) best = k == k0 ? len[k] : best;
+    float t = cost((float)best, (float)(wgs * p.n_kv_heads), p.cost_once + p.cost_piece, 0.125f) + p.cost_merge;
+    if (best >= most || wgs > p.max_items) t = INFINITY;
+#pragma unroll
+    for (int d = kPlanLengths / 2; d > 0; d /= 2) {
+      const float t2 = __shfl_xor(t, d);
+      const int best2 = __shfl_xor(best, d);
+      if (t2 < t || (t2 == t && best2 > best)) t = t2, best = best2;
+    }
     const float whole = cost((float)most, (float)(all.blocks * p.n_kv_heads), p.cost_once, 0.5f);
-    // in the lanes: a place's share, and half as much again
-    const int j = 2 + (l & 1), least = (most + p.n_pieces - 1) / p.n_pieces;
-    int len = (int)fminf(ceilf(work * (float)j / (2.f * places)), 1e9f);
-    len = len < least ? least : len;
-    len = len < p.shortest ? p.shortest : len;
-    len = (len + p.step - 1) / p.step * p.step;
-    const float wgs = ((float)all.tiles / (float)len + 0.5f * (float)all.blocks) * (float)p.n_kv_heads;
-    float t = cost((float)len, wgs, p.cost_once + p.cost_piece, 0.125f) + p.cost_merge;
-    if (len >= most) t = INFINITY;
-    const float t2 = __shfl_xor(t, 1);
-    const int len2 = __shfl_xor(len, 1);
-    if (t2 < t || (t2 == t && len2 > len)) t = t2, len = len2;
-    if (t < whole) piece = len;
+    if (t < whole) piece = best;
   }
 
   // ---- the items: counted by classes, then written
@@ -301,7 +334,7 @@ __device__ void prompt_plan(const PromptPlanParams& p) {
       }
     }
   };
-  int total = 0;
+  int total;
   for (;;) {
     for (int s0 = 0; s0 < p.n_seqs; s0 += NT) {
       PlanSums y = all;
