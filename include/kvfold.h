@@ -491,7 +491,11 @@ int kvfold_pcache_assign(const kvfold_pcache_t* cache, int32_t n_seqs, const int
                          int32_t* tables, int64_t table_stride, int32_t* lens_after, int32_t* cu_new, int64_t* slots, int32_t* positions, int64_t n_slots,
                          int32_t* n_free_after, int32_t* status, void* stream);
 
-/* A batch: sequence s has the new tokens cu_new[s] .. cu_new[s + 1] - 1 of the packed rows, the last of its lens[s] tokens. */
+/*
+ * A batch: sequence s has the new tokens cu_new[s] .. cu_new[s + 1] - 1 of the packed rows, the last of its lens[s] tokens.  Sequences whose tokens overlap have no
+ * defined results.  n_seqs <= 2^20, n_seqs * n_kv_heads <= 2^23, n_tokens * n_q_heads <= 2^28, n_tokens * q_stride <= 2^34, table_stride < 2^31, kv_stride <= 2^31, else
+ * KVFOLD_ERR_UNSUPPORTED.
+ */
 typedef struct {
   uint32_t struct_size;  /* must be sizeof(kvfold_batch_t)                                                                      */
   int32_t n_seqs;        /* >= 0                                                                                                */

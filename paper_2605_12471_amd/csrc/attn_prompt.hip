@@ -1273,69 +1273,73 @@ hipError_t launch_attn_prompt(const PAttnParams& p, int head_dim, bool bf16, int
 template <class T, int D>
 __global__ void __launch_bounds__(256) pmerge_kernel(PAttnParams p, int parts_log2) {
   constexpr int V = D / 4, ROWS = 256 / V, N = 8;  // (unit_rows / ROWS = 2^parts_log2 workgroups share a block's rows)
-  const unsigned id = blockIdx.x >> parts_log2;
-  const int at_block = (int)quot(id, p.by_kv_heads);
-  if (at_block >= ((ConstPtr<int32_t>)(uintptr_t)p.list_head)[1]) return;
-  const PromptWork wk = prompt_item(p, ((ConstPtr<int32_t>)(uintptr_t)p.merges)[at_block], (int)id - at_block * p.n_kv_heads);
-  const int n = wk.n_pieces, c = threadIdx.x % V, r = wk.row0 + (int)(blockIdx.x & ((1u << parts_log2) - 1)) * ROWS + (int)threadIdx.x / V;
-  if (r >= wk.rows) return;
-  const unsigned place = prompt_place(p, wk, r), Hq = (unsigned)p.n_q_heads;
-  const int64_t n_rows = (int64_t)p.n_tokens * Hq;
-  float M = -INFINITY, L = 0.f;
-  floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+  const unsigned todo = ((unsigned)((ConstPtr<int32_t>)(uintptr_t)p.list_head)[1] * (unsigned)p.n_kv_heads) << parts_log2;
 #pragma unroll 1
-  for (int i0 = 0; i0 < n; i0 += N) {
-    floatx2 ml[N];
-    floatx4 o[N];
+  for (unsigned id = blockIdx.x; id < todo; id += gridDim.x) {
+    const int at_block = (int)quot(id >> parts_log2, p.by_kv_heads);
+    const PromptWork wk = prompt_item(p, ((ConstPtr<int32_t>)(uintptr_t)p.merges)[at_block], (int)(id >> parts_log2) - at_block * p.n_kv_heads);
+    const int n = wk.n_pieces, c = threadIdx.x % V, r = wk.row0 + (int)(id & ((1u << parts_log2) - 1)) * ROWS + (int)threadIdx.x / V;
+    if (r >= wk.rows) continue;
+    const unsigned place = prompt_place(p, wk, r), Hq = (unsigned)p.n_q_heads;
+    const int64_t n_rows = (int64_t)p.n_tokens * Hq;
+    float M = -INFINITY, L = 0.f;
+    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int i0 = 0; i0 < n; i0 += N) {
+      floatx2 ml[N];
+      floatx4 o[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int64_t part = (int64_t)(i0 + i < n ? i0 + i : n - 1) * n_rows + place;
-      ml[i] = *reinterpret_cast<const floatx2*>(p.part_ml + part * 2);
-      o[i] = *reinterpret_cast<const floatx4*>(p.part_o + part * D + c * 4);
-    }
-    float top = M;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      if (i0 + i >= n || ml[i].y == 0.f) {  // no key for the row in this piece
-        ml[i] = floatx2{-INFINITY, 0.f};
-        o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < N; ++i) {
+        const int64_t part = (int64_t)(i0 + i < n ? i0 + i : n - 1) * n_rows + place;
+        ml[i] = *reinterpret_cast<const floatx2*>(p.part_ml + part * 2);
+        o[i] = *reinterpret_cast<const floatx4*>(p.part_o + part * D + c * 4);
       }
-      top = fmaxf(top, ml[i].x);
+      float top = M;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if (i0 + i >= n || ml[i].y == 0.f) {  // no key for the row in this piece
+          ml[i] = floatx2{-INFINITY, 0.f};
+          o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+        }
+        top = fmaxf(top, ml[i].x);
+      }
+      const float ref = top == -INFINITY ? 0.f : top, f0 = __builtin_amdgcn_exp2f(M - ref);
+      M = top;
+      L *= f0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] *= f0;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float f = __builtin_amdgcn_exp2f(ml[i].x - ref);
+        L = __builtin_fmaf(ml[i].y, f, L);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(o[i][e], f, acc[e]);
+      }
     }
-    const float ref = top == -INFINITY ? 0.f : top, f0 = __builtin_amdgcn_exp2f(M - ref);
-    M = top;
-    L *= f0;
+    const float inv = 1.f / L;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] *= f0;
+    for (int e = 0; e < 4; ++e) acc[e] = L == 0.f ? 0.f : acc[e] * inv;
+    const uint64_t at = (uint64_t)place * D + (unsigned)c * 4u;
+    if constexpr (sizeof(T) == 2) {
+      bf16x4 v;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float f = __builtin_amdgcn_exp2f(ml[i].x - ref);
-      L = __builtin_fmaf(ml[i].y, f, L);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(o[i][e], f, acc[e]);
+      for (int e = 0; e < 4; ++e) v[e] = (__bf16)acc[e];
+      *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p.out) + at) = v;
+    } else {
+      *reinterpret_cast<floatx4*>(static_cast<float*>(p.out) + at) = acc;
     }
+    const unsigned token = place / Hq;
+    if (p.lse && c == 0) p.lse[(int64_t)(place - token * Hq) * p.n_tokens + token] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * 0.6931471805599453f;
   }
-  const float inv = 1.f / L;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) acc[e] = L == 0.f ? 0.f : acc[e] * inv;
-  const uint64_t at = (uint64_t)place * D + (unsigned)c * 4u;
-  if constexpr (sizeof(T) == 2) {
-    bf16x4 v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = (__bf16)acc[e];
-    *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p.out) + at) = v;
-  } else {
-    *reinterpret_cast<floatx4*>(static_cast<float*>(p.out) + at) = acc;
-  }
-  const unsigned token = place / Hq;
-  if (p.lse && c == 0) p.lse[(int64_t)(place - token * Hq) * p.n_tokens + token] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * 0.6931471805599453f;
 }
 
 hipError_t launch_pmerge(const PAttnParams& p, int head_dim, bool bf16, hipStream_t s) {
   const int rows = 256 / (head_dim / 4);
   int lg = 0;
   while (rows << lg < p.unit_rows) ++lg;
-  const dim3 grid(((unsigned)p.n_blocks * (unsigned)p.n_kv_heads) << lg), block(256);
+  // (how many blocks there are to merge only the device knows: no more workgroups than find out at once, 32 a CU)
+  const unsigned most = ((unsigned)p.n_blocks * (unsigned)p.n_kv_heads) << lg, cap = 32u * (unsigned)p.n_cu;
+  const dim3 grid(most < cap ? most : cap), block(256);
   if (bf16 && head_dim == 128)
     hipLaunchKernelGGL((pmerge_kernel<__bf16, 128>), grid, block, 0, s, p, lg);
   else if (bf16)

@@ -123,7 +123,7 @@ struct PAttnParams {
   int32_t n_q_heads, n_kv_heads, group, page_log2, n_pages;
   int32_t n_pieces, piece, unit_rows;
   int32_t n_units;   // decode: sequences times KV heads; prompts: items at most
-  int32_t n_blocks;  // prompts: blocks of rows, at most
+  int32_t n_blocks, n_cu;  // prompts: blocks of rows, at most
   int32_t from_end;  // decode: PagedPlan
   float scale_log2e, from_log2, stale;  // its reciprocal, and 2^16 in its units
   FastDiv by_group, by_units, by_kv_heads;

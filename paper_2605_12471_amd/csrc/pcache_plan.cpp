@@ -33,7 +33,7 @@ int validate_batch(const kvfold_pcache_config_t& c, const kvfold_batch_t* b) {
   const int64_t unit = 16 / elem_size(c.dtype), wide = (int64_t)c.n_q_heads * c.head_dim, narrow = (int64_t)c.n_kv_heads * c.head_dim;
   if (b->q_stride % unit || b->kv_stride % unit || (b->q_stride && b->q_stride < wide) || (b->kv_stride && b->kv_stride < narrow)) return KVFOLD_ERR_INVALID_ARG;
   if (b->max_len > (int64_t)1 << 30 || b->table_stride >= (int64_t)1 << 31 || (int64_t)b->n_tokens * c.n_q_heads > (int64_t)1 << 28 || b->n_seqs > 1 << 20 ||
-      (int64_t)b->n_seqs * c.n_kv_heads > (int64_t)1 << 24 || b->kv_stride > (int64_t)1 << 31 || (b->q_stride >> 3) > ((int64_t)1 << 31) / std::max(b->n_tokens, 1))
+      (int64_t)b->n_seqs * c.n_kv_heads > (int64_t)1 << 23 || b->kv_stride > (int64_t)1 << 31 || (b->q_stride >> 3) > ((int64_t)1 << 31) / std::max(b->n_tokens, 1))
     return KVFOLD_ERR_UNSUPPORTED;
   return KVFOLD_OK;
 }

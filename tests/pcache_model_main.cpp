@@ -152,14 +152,14 @@ static void plans() {
     for (int type : {KVFOLD_BF16, KVFOLD_F32}) {
       const kvfold_pcache_config_t c = config(32, 8, d, 16, (1 << 27) - 1, type);
       CHECK(validate_pconfig(&c) == KVFOLD_OK);
-      for (int seqs : {1, 1 << 20})
+      for (int seqs : {1, 1 << 20})  // (times 8 KV heads: as many as there may be)
         for (int tokens : {1, 1 << 20, 1 << 23})
           for (int max_new : {1, 4, 100, 1 << 23})
             for (int64_t len : {(int64_t)1, (int64_t)5000, (int64_t)1 << 30}) {
               const kvfold_batch_t b = batch(seqs, tokens, max_new, len, 1 << 26);
               CHECK(validate_batch(c, &b) == KVFOLD_OK);
               const PagedPlan pl = make_pplan(c, 256, b);
-              CHECK(pl.rows >= 0 && pl.rows <= kPagedMaxRows && pl.bytes >= pl.counters && pl.bytes < (size_t)1 << 36 && pl.items < (int64_t)1 << 31);
+              CHECK(pl.rows >= 0 && pl.rows <= kPagedMaxRows && pl.bytes >= pl.counters && pl.bytes < (size_t)1 << 36 && pl.items * 8 < (int64_t)1 << 24);  // (256 threads each: below 2^32)
               CHECK(pl.n_pieces >= 1 && (!pl.decode || (pl.piece >= 128 && (int64_t)pl.piece * pl.n_pieces >= std::min<int64_t>(len, 1 << 30))));
             }
     }
