@@ -66,13 +66,12 @@ constexpr float kRedoThreshold = 1152921504606846976.0f;  // 2^60: beyond this t
 //   * exp2 / pack / row-sum "events" of half hh (one event = one exp2; the second event of a logit
 //     pair also packs the pair, and each event adds the exp2 before it to the row sum): events
 //     [NEAR, NE) in slots [0, EW) of the half's own step, so that slab 0 of P is packed before phase
-//     2 and slab 1 before its second half; with SUM_MODE the first NEAR events (all in slab 0) are
+//     2 and slab 1 before its second half; the first NEAR events (all in slab 0) are
 //     taken EARLY, in the tail slots [EW, M) of the step before, as soon as that S^T is complete;
 //   * LDS fragment reads one batch ahead, in slots [0, RW), RW half way into the tail, one wait per batch;
-//   * SUM_MODE: the test of the row sums against 2^20 right after the last event; else the row
-//     maxima of half hh+1 and the rescale decision in the exp-free tail [RM0, M);
+//   * the test of the row sums against 2^20 right after the last event (no row maximum is taken below the causal horizon);
 //   * in odd steps the workgroup barrier and the ring refill (DMA) in the tail [EW, M).
-template <int D, int QA, bool SUM_MODE, int LPG>
+template <int D, int QA, int LPG>
 struct PromptSched {
   static constexpr int KS = D / 16, DB = D / 32;
   static constexpr int M1 = KS * QA;       // MFMAs of phase 1 (K fragment ks feeds QA of them)
@@ -81,7 +80,7 @@ struct PromptSched {
   static constexpr int NP = QA * 8;        // logit pairs per step; pair k: slab k / (4 QA), unit (k / 4) % QA
   static constexpr int NE = 2 * NP;        // exp events
   static constexpr int EW = M1 + M2 / 2;
-  static constexpr int NEAR = SUM_MODE ? (NE * (M - EW) / M) & ~1 : 0;
+  static constexpr int NEAR = (NE * (M - EW) / M) & ~1;
   static constexpr int NMAIN = NE - NEAR;
   static_assert(NEAR <= NE / 2, "early events must stay inside slab 0");
   static_assert(NEAR + (M1 * NMAIN + EW - 1) / EW >= NE / 2, "slab 0 would not be complete at the start of phase 2");
@@ -91,10 +90,6 @@ struct PromptSched {
                                              //   kg[1] (GK) | vg[0] (2 GV) | vg[1] (2 GV) | kg[0] of the next step (GK)
   static constexpr int RW = EW + (M - EW) / 2;  // (measured: spreading the reads a little into the tail beats stopping at EW)
   static_assert(EW + 1 < M, "no slot for the row-sum test");
-  static constexpr int RM1 = M - 1 - QA;   // row-max slots [RM0, RM1), then QA + 1 decision slots
-  static constexpr int RM0 = (EW - (M >= 32 ? 2 : 0)) < RM1 ? (EW - (M >= 32 ? 2 : 0)) : RM1 - 1;
-  static_assert(SUM_MODE || RM0 >= M1 + 1, "row maxima would read S^T before its MFMAs retire");
-  static_assert(SUM_MODE || (RM1 > RM0 && RM1 + QA < M), "no room for the row maxima");
   static_assert(LPG <= (M - EW) * 4, "ring refill does not fit the tail");
   // read r is issued in slot r * RW / R; reads issued before slot sl:
   static constexpr int rd_before(int sl) {
@@ -243,7 +238,6 @@ constexpr int prompt_lds = (2 * kPromptRing + 1) * kTileKeys * D * 2;
 template <int D>
 __global__ void __launch_bounds__(256, 1) attn_prompt_kernel(PAttnParams p) {
   constexpr int QB = 2, NV = kPromptRing;
-  constexpr bool SUM_MODE = true;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const unsigned lds0 = (unsigned)(uintptr_t)((unsigned char __attribute__((address_space(3)))*)smem);
   constexpr int NK = NV + 1;         // K ring slots (K runs half a tile ahead of V in the pipeline)
@@ -635,7 +629,7 @@ __global__ void __launch_bounds__(256, 1) attn_prompt_kernel(PAttnParams p) {
   // the early events of a half all at once (prologue, masked steps, and again after a sum-driven shift)
   auto early_events = [&](const floatx16 (&s)[QB], auto q0_tag) __attribute__((always_inline)) {
     constexpr int Q0 = decltype(q0_tag)::value, QA = QB - Q0;
-    constexpr int NEAR = PromptSched<D, QA, SUM_MODE, LPG>::NEAR;
+    constexpr int NEAR = PromptSched<D, QA, LPG>::NEAR;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) lsum_early[qb] = 0.f;
     if (NEAR > 0) {
@@ -667,9 +661,9 @@ __global__ void __launch_bounds__(256, 1) attn_prompt_kernel(PAttnParams p) {
     constexpr bool ODD = decltype(odd_tag)::value;
     constexpr bool MASKED = decltype(masked_tag)::value;
     constexpr int Q0 = decltype(q0_tag)::value, QA = QB - Q0;
-    using S = PromptSched<D, QA, SUM_MODE, LPG>;
-    constexpr int M1 = S::M1, M = S::M, EW = S::EW, NE = S::NE, NEAR = S::NEAR, NMAIN = S::NMAIN, NP = S::NP;
-    constexpr int R = S::R, RW = S::RW, RM0 = S::RM0, RM1 = S::RM1;
+    using S = PromptSched<D, QA, LPG>;
+    constexpr int M1 = S::M1, M = S::M, EW = S::EW, NE = S::NE, NEAR = S::NEAR, NMAIN = S::NMAIN;
+    constexpr int R = S::R, RW = S::RW;
     const int t = hh >> 1;
     constexpr int KIMM = ODD ? 0 : HALFB;  // even hh: half hh+1 is the second half of tile t
     constexpr int VIMM = ODD ? HALFB : 0;  // even hh: half hh is the first half of tile t
@@ -683,7 +677,7 @@ __global__ void __launch_bounds__(256, 1) attn_prompt_kernel(PAttnParams p) {
     bool need_rescale = false;
     int sum_flag = 0;      // per lane: a row sum of this half passed 2^20 (or is not a number)
     int kslot_prev = 0, vslot_prev = 0;
-    const bool more = (SUM_MODE ? PLAIN : !ODD) || hh + 1 < 2 * t_end;  // half hh + 1 is there (or nothing is decided on it)
+    const bool more = PLAIN || hh + 1 < 2 * t_end;  // half hh + 1 is there (or nothing is decided on it)
 
     wait_lds<0>();  // kg[0] (fetched at the end of the previous step) has landed
     // the page that the next (odd) step's copies of K come from: there by its own wait
@@ -698,7 +692,7 @@ __global__ void __launch_bounds__(256, 1) attn_prompt_kernel(PAttnParams p) {
       if (ODD && i == EW) {
         // Every read of K[t] and V[t] by this wave has returned.  K[t+2] and V[t+1] were issued
         // NV-1 tiles ago: they are the oldest group in flight.
-        if (PLAIN || (NV > 2 && t + NV < t_end && t + NV < t_whole))
+        if (PLAIN || (t + NV < t_end && t + NV < t_whole))
           wait_vm<(NV - 2) * LPG>();
         else
           wait_vm<0>();  // the group issued last is not whole
@@ -757,23 +751,10 @@ __global__ void __launch_bounds__(256, 1) attn_prompt_kernel(PAttnParams p) {
           exp_event(s_next, lsum_next, j, j == 0, q0_tag);
         if (i == M - 1) lsum_next[ev_unit(NEAR - 1, Q0, QA)] += ev_b;
       }
-      if (SUM_MODE && i == EW + 1) {
+      if (i == EW + 1) {
 #pragma unroll
         for (int qb = Q0; qb < QB; ++qb) sum_flag |= (int)!(lsum[qb] <= kSumThreshold);
       }
-      // row maxima of half hh+1 (its last MFMA is at least RM0 - M1 slots old), then the decision
-      if (!SUM_MODE && !MASKED && i >= RM0 && i < RM1) {
-#pragma unroll
-        for (int k = ((i - RM0) * NP) / (RM1 - RM0); k < ((i - RM0 + 1) * NP) / (RM1 - RM0); ++k) {
-          const int q2 = Q0 + (k >> 3), r = 2 * (k & 7);
-          if (r == 0)
-            mx[q2] = fmaxf(s_next[q2][0], s_next[q2][1]);
-          else
-            mx[q2] = fmaxf(fmaxf(mx[q2], s_next[q2][r]), s_next[q2][r + 1]);
-        }
-      }
-      if (!SUM_MODE && !MASKED && i >= RM1 && i < RM1 + QA) dm[Q0 + i - RM1] = pair_max(mx[Q0 + i - RM1]);
-      if (!SUM_MODE && !MASKED && i == RM1 + QA) need_rescale = rescale_need(dm, Q0);
       // ring refill and the V address of the next tile (odd steps, after the barrier)
       if (ODD && i >= EW) {
         if (PLAIN) {
@@ -799,13 +780,11 @@ __global__ void __launch_bounds__(256, 1) attn_prompt_kernel(PAttnParams p) {
       l_run[qb] += lsum[qb];
       lsum_early[qb] = lsum_next[qb];
     }
-    if constexpr (SUM_MODE) {
-      if (__builtin_expect(__any(sum_flag), 0)) {
+    if (__builtin_expect(__any(sum_flag), 0)) {
 #pragma unroll
-        for (int qb = Q0; qb < QB; ++qb) mfma_settle_v(s_next[qb]);
-        rescale_from_sum(lsum, s_next, Q0);  // (past the last half s_next is stale, and merely moved)
-        if (!MASKED) early_events(s_next, q0_tag);  // they were formed against the old reference: once more
-      }
+      for (int qb = Q0; qb < QB; ++qb) mfma_settle_v(s_next[qb]);
+      rescale_from_sum(lsum, s_next, Q0);  // (past the last half s_next is stale, and merely moved)
+      if (!MASKED) early_events(s_next, q0_tag);  // they were formed against the old reference: once more
     }
     if (!PLAIN && ODD) {
       issue_tile(false, t + 1 + NV, kslot_prev);
@@ -819,17 +798,12 @@ __global__ void __launch_bounds__(256, 1) attn_prompt_kernel(PAttnParams p) {
       need_rescale = rescale_decide(mx, dm, Q0);
     }
     if (__builtin_expect(need_rescale, 0)) {
-      // One-unit kernel: `more` is looked at in here; as part of the branch its scalar instructions ended every step
-      // (C = 128 on 32K keys, 28 heads on 4: 145 us with them, 141 without).
-      if (!SUM_MODE && !MASKED) asm volatile("");
-      if (SUM_MODE || MASKED || more) {
 #pragma unroll
-        for (int qb = Q0; qb < QB; ++qb) mfma_settle_v(s_next[qb]);
-        rescale_apply(dm, s_next, Q0);
-      }
+      for (int qb = Q0; qb < QB; ++qb) mfma_settle_v(s_next[qb]);
+      rescale_apply(dm, s_next, Q0);
     }
     if (MASKED) {
-      if (QB == 2 && Q0 == 0 && next_unit1_only)
+      if (Q0 == 0 && next_unit1_only)
         early_events(s_next, std::integral_constant<int, QB - 1>{});
       else
         early_events(s_next, q0_tag);
@@ -847,10 +821,10 @@ __global__ void __launch_bounds__(256, 1) attn_prompt_kernel(PAttnParams p) {
       if (!exact && t_end * BN <= vis_min) t_fast = t_end;  // the piece ends below every horizon
       if (t_fast > t_end) t_fast = t_end;
       if (t_fast > t_bad - 1) t_fast = t_bad - 1;  // (pages that are none are masked)
-      // Two-unit kernel: from tile t_dead on every key is beyond the last row of unit 0 and only unit 1
+      // From tile t_dead on every key is beyond the last row of unit 0 and only unit 1
       // is worked on, fast up to its own horizon (t_fast1), masked from there.
       int t_dead = vis_last0 > 0 ? (vis_last0 + BN - 1) / BN : 0;
-      if (QB == 1 || exact || t_dead > t_end) t_dead = t_end;
+      if (exact || t_dead > t_end) t_dead = t_end;
       int t_fast1 = (vis_first[QB - 1] - 96) / BN + 1;
       if (vis_first[QB - 1] < 96 || exact) t_fast1 = 0;
       if (t_fast1 > t_end) t_fast1 = t_end;
@@ -871,7 +845,7 @@ __global__ void __launch_bounds__(256, 1) attn_prompt_kernel(PAttnParams p) {
       if (idle) {
         // no rows of its own: this wavefront only moves its share of the tiles
         for (int t = t_begin, ks = 0, vs = 0; t < t_end; ++t) {
-          if (NV > 2 && t + NV < t_end && t + NV < t_whole)
+          if (t + NV < t_end && t + NV < t_whole)
             wait_vm<(NV - 2) * LPG>();
           else
             wait_vm<0>();
@@ -907,7 +881,7 @@ __global__ void __launch_bounds__(256, 1) attn_prompt_kernel(PAttnParams p) {
         float mx[QB];
         rowmax_all(sA, mx);
         reference_first(mx, sA);
-        if (QB == 2 && t_begin >= t_dead && t_dead < t_end)
+        if (t_begin >= t_dead && t_dead < t_end)
           early_events(sA, std::integral_constant<int, QB - 1>{});  // the first step already works on unit 1 alone
         else
           early_events(sA, std::integral_constant<int, 0>{});
@@ -935,23 +909,21 @@ __global__ void __launch_bounds__(256, 1) attn_prompt_kernel(PAttnParams p) {
           step(sA, sB, 2 * t, even, masked, mixed, both);
           step(sB, sA, 2 * t + 1, odd, masked, mixed, both, t + 1 == t_dead && t_dead < t_end);
         }
-        if constexpr (QB == 2) {
-          // unit 0 is done for good (every further key is beyond its last row): unit 1 alone
-          constexpr std::integral_constant<int, 1> second{};
-          for (; t < t_fast1; ++t) {
-            step(sA, sB, 2 * t, even, unmasked, mixed, second);
-            step(sB, sA, 2 * t + 1, odd, unmasked, mixed, second);
-          }
-          for (; t < t_end; ++t) {
-            step(sA, sB, 2 * t, even, masked, mixed, second);
-            step(sB, sA, 2 * t + 1, odd, masked, mixed, second);
-          }
+        // unit 0 is done for good (every further key is beyond its last row): unit 1 alone
+        constexpr std::integral_constant<int, 1> second{};
+        for (; t < t_fast1; ++t) {
+          step(sA, sB, 2 * t, even, unmasked, mixed, second);
+          step(sB, sA, 2 * t + 1, odd, unmasked, mixed, second);
+        }
+        for (; t < t_end; ++t) {
+          step(sA, sB, 2 * t, even, masked, mixed, second);
+          step(sB, sA, 2 * t + 1, odd, masked, mixed, second);
         }
       }
       wait_vm<0>();  // nothing of ours may still be writing LDS when the workgroup retires or starts over
       wait_lds<0>();
       __syncthreads();  // every wavefront of the workgroup is through with the rings
-      if (!SUM_MODE || exact) break;
+      if (exact) break;
       // Did a row sum of any wavefront overflow?
       if (lane_now() == 0) *LDS_PTR(int, lds0 + 4u * (unsigned)w) = overflowed;
       __syncthreads();

@@ -260,3 +260,9 @@ def test_pages_far_into_a_large_cache(dtype):
             for to, rows in zip(large.view(1), small.cache.view(0)):
                 assert torch.equal(to[far.cuda()].nan_to_num(3), rows.nan_to_num(3))
             small.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_blocks_to_merge_than_a_launch_has_workgroups_for(dtype):
+    """A long sequence beside many short ones, all of them cut: the merge goes through its list in turns."""
+    Fold(16, 8, 128, 16, [5000] * 20 + [600] * 70, [40] * 90, dtype, pad=1).step().check().check_pages()
