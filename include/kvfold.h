@@ -528,7 +528,7 @@ size_t kvfold_pcache_workspace_bytes(const kvfold_pcache_t* cache, const kvfold_
  *          A row that sees no key, or whose logits are all -inf, gets zeros and -inf.
  *   workspace  device, 256-byte aligned, at least kvfold_pcache_workspace_bytes() bytes, else KVFOLD_ERR_OOM
  * A row that the call stores may be seen by one sequence of the batch.  out, lse and the workspace lie apart from all else, and nothing in the cache's
- * storage, else KVFOLD_ERR_INVALID_ARG.  The same call gives the same bits.
+ * storage, else KVFOLD_ERR_INVALID_ARG.  The same call gives the same bits; beside other sequences a row's may be others, within the rounding (its keys are cut elsewhere).
  */
 int kvfold_pcache_step(const kvfold_pcache_t* cache, int layer, const kvfold_batch_t* batch /* host */, const void* q, const void* k_new, const void* v_new,
                        void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);

@@ -29,6 +29,17 @@ typedef __attribute__((ext_vector_type(2))) float floatx2;
 
 constexpr int kPDecodeWaves = 4;  // (eight: never better, 300 keys 9.6 us for 8.8, 64 sequences of 500 31 for 26)
 
+// The sum of the wavefront's values, for all its lanes
+__device__ __forceinline__ int wave_sum(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);  // lanes 1, 2, 4 and 8 down in the row of 16,
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, true);  // a row's last lane to the next row, of two
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, true);  // and lane 31 to the upper half
+  return __builtin_amdgcn_readlane(x, 63);
+}
+
 template <class T, int D>
 __global__ void __launch_bounds__(kPDecodeWaves * 64, 2) attn_pdecode_kernel(PAttnParams p) {
   constexpr bool BF16 = sizeof(T) == 2;
@@ -48,14 +59,16 @@ __global__ void __launch_bounds__(kPDecodeWaves * 64, 2) attn_pdecode_kernel(PAt
 
   // (every line of the arguments is fetched now, in one round trip)
   asm volatile("" ::"s"(p.q), "s"(p.out), "s"(p.slots), "s"(p.table_stride), "s"(p.n_seqs), "s"(p.n_pieces), "s"(p.by_kv_heads.mul));
-  // The longest sequences' last pieces first, which are whole; everybody's first one, which is what is left of its length, at the end.
-  const int n_before = (int)quot(blockIdx.x, p.by_units), unit = (int)blockIdx.x - n_before * p.n_units, piece = p.n_pieces - 1 - n_before;
+  // The longest sequences' last pieces first (from_end), which are whole; everybody's first one, which is what is left of its length, at the end.  Else everybody's first piece, and so
+  // on: pieces that are not there, of which there are many where lengths decide, would hold up the others in front of them (8 equal sequences of 4000 keys 31.0 us, so 26.7).
+  const int n_before = (int)quot(blockIdx.x, p.by_units), unit = (int)blockIdx.x - n_before * p.n_units, piece = p.from_end ? p.n_pieces - 1 - n_before : n_before;
   const int seq = (int)quot((unsigned)unit, p.by_kv_heads), g = unit - seq * p.n_kv_heads;
   const int tid = threadIdx.x, l = tid & 63, kg = l >> 4, c16 = l & 15;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int32_t* table = p.tables + (int64_t)seq * p.table_stride;
   int pages[TILES];  // lane l: of the wavefront's block (the last multiple of 64) + l
-  if (!p.from_end) {  // where a piece begins is known: its pages are asked for together with the lengths (a tenth of the time of a short sequence's step)
+  const bool known = !p.from_end && p.shared == 0.f;
+  if (known) {  // where a piece begins is known: its pages are asked for together with the lengths (a tenth of the time of a short sequence's step)
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
       const int64_t column = (((int64_t)piece * (p.piece / BK) + w + NW * l) * BK + 16 * t) >> p.page_log2;
@@ -72,14 +85,24 @@ __global__ void __launch_bounds__(kPDecodeWaves * 64, 2) attn_pdecode_kernel(PAt
     }
     sq = paged_seq(from, to, len, p.n_tokens, p.max_new, p.max_len);
   }
-  const int n_pieces = paged_pieces(sq.len, p.piece);
+  int piece_keys = p.piece;
+  if (p.shared != 0.f) {  // a workgroup's share of all keys: every workgroup adds up all lengths, which come with its own
+    int steps = 0;        // (of 128 keys: a sum of fewer than 2^31)
+    for (int s = l; s < p.n_seqs; s += 64) {
+      const int len = p.lens[s];
+      steps += (int)((unsigned)(len < 0 ? 0 : len > p.max_len ? p.max_len : len) + 127u) / 128;
+    }
+    const int share = (int)fminf(ceilf((float)wave_sum(steps) * p.shared), (float)(kPagedLongestPiece / 128)) * 128;
+    piece_keys = share > piece_keys ? share : piece_keys;
+  }
+  const int n_pieces = paged_pieces(sq.len, piece_keys);
   if (sq.n == 0 || piece >= n_pieces) return;
 
   const int Hq = p.n_q_heads, G = p.group, rows = sq.n * G, prev = sq.len - sq.n;
 
   // ---- the wavefront's blocks: every NW-th of the piece's.  New rows lie in the sequence's last two at most, so that a wavefront has at most one with new
   // rows, its last.
-  const int b_all = (sq.len + BK - 1) / BK, per_piece = p.piece / BK;
+  const int b_all = (sq.len + BK - 1) / BK, per_piece = piece_keys / BK;
   int b_begin = piece * per_piece, b_end = b_begin + per_piece < b_all ? b_begin + per_piece : b_all;
   if (p.from_end) {  // what is left of the length is the first piece's
     b_end = b_all - (n_pieces - 1 - piece) * per_piece;
@@ -102,7 +125,7 @@ __global__ void __launch_bounds__(kPDecodeWaves * 64, 2) attn_pdecode_kernel(PAt
       if (!mine) pages[t] = -1;
     }
   };
-  fetch_pages(0, !p.from_end);
+  fetch_pages(0, known);
 
   // ---- Q: lane (c16, kg) holds the columns of row c16 that its shares of the K rows have
   const int row = c16 < rows ? c16 : rows - 1, tok = (int)quot((unsigned)row, p.by_group);

@@ -11,6 +11,8 @@ namespace kvfold {
 constexpr int64_t kPagedMaxRows = 1 << 20;  // (row, piece) pairs of a workspace
 constexpr int kPagedMeetStride = 16;        // words from one unit's counter to the next: a line's
 constexpr int kPagedMaxPieces = 128;        // of a sequence's keys
+constexpr int kPagedLongestPiece = 2048;    // keys (decode)
+constexpr int64_t kPagedMostWgs = 2048;     // of a decoding step whose lengths decide: many find that they have no piece (4096: 27.1 us for the first 24.2 in pcache_plan.cpp, 1024: 27.0)
 
 int validate_pconfig(const kvfold_pcache_config_t* c);
 size_t pcache_layer_bytes(const kvfold_pcache_config_t& c);  // K and V
@@ -26,7 +28,8 @@ struct PagedPlan {
   int places, shortest, step;  // PromptPlanParams
   float cost_once, cost_piece, cost_merge;
   int n_pieces;          // of the keys, at most
-  int piece;             // decode: keys of one, a multiple of 128
+  int piece;             // decode: keys of one, a multiple of 128; where lengths decide, the fewest
+  float shared;          // decode: steps of 128 keys of a piece for each that the sequences have, together; 0: the lengths do not decide
   int64_t rows;          // of partial results
   size_t counters;       // bytes in front of them: of the counters by which pieces meet,
   size_t list;           // prompts: and of the work's list
@@ -124,7 +127,8 @@ struct PAttnParams {
   int32_t n_pieces, piece, unit_rows;
   int32_t n_units;   // decode: sequences times KV heads; prompts: items at most
   int32_t n_blocks, n_cu;  // prompts: blocks of rows, at most
-  int32_t from_end;  // decode: PagedPlan
+  int32_t from_end;  // decode: PagedPlan,
+  float shared;      // as here
   float scale_log2e, from_log2, stale;  // its reciprocal, and 2^16 in its units
   FastDiv by_group, by_units, by_kv_heads;
 };

@@ -232,6 +232,7 @@ int kvfold_pcache_step(const kvfold_pcache_t* c, int layer, const kvfold_batch_t
   p.n_blocks = (int32_t)pl.blocks;
   p.n_cu = c->n_cu;
   p.from_end = pl.from_end;
+  p.shared = pl.shared;
   p.part_o = reinterpret_cast<float*>(list + pl.list);
   p.part_ml = p.part_o + pl.rows * f.head_dim;
   p.table_stride = b->table_stride;

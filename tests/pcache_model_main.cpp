@@ -121,6 +121,7 @@ static void plans() {
       CHECK(pl.unit_rows <= 16 && pl.unit_rows >= std::min(max_new, tokens) * G && pl.piece % 128 == 0 && pl.n_pieces <= kPagedMaxPieces);
       for (int s = 0; s < seqs; ++s) CHECK(paged_pieces(len[s], pl.piece) <= pl.n_pieces);
       CHECK(pl.n_pieces == 1 || pl.rows == (int64_t)seqs * h[1] * pl.n_pieces * pl.unit_rows);
+      CHECK(pl.shared == 0.f || (!pl.from_end && seqs > 1 && (int64_t)seqs * h[1] < 256 && (int64_t)seqs * h[1] * pl.n_pieces <= 2 * kPagedMostWgs));  // (pieces are longer than pl.piece then)
       continue;
     }
     ++prompts;
