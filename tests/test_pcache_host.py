@@ -1,5 +1,6 @@
 """Host side of the cache in pages: refusals, bytes, plans, and the reference's own rules, none of which needs a GPU."""
 import os
+import re
 import subprocess
 
 import numpy as np
@@ -8,7 +9,7 @@ import torch
 
 import paper_2605_12471_amd as kv
 import pcache_ref as R
-from paper_2605_12471_amd import binding
+from paper_2605_12471_amd import binding, build
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -81,3 +82,30 @@ def test_the_reference_itself():
     assert (out[1] == 0).all() and np.isneginf(lse[:, 1]).all() and np.isfinite(lse[:, [0, 2]]).all()
     assert R.assign([3, 0, 16], [1, 17, 1], [9, 8, 7, 6], 4, [[1, -1], [-1, -1], [2, -1]], 16, 21) == (
         [[1, -1], [6, 7], [2, 8]], [4, 17, 17], [0, 1, 18, 19], [19] + list(range(96, 112)) + [112, 128, -1, -1], [3] + list(range(17)) + [16, -1, -1], 1, 0)
+
+
+def test_what_matrix_instructions_written_by_hand_read_is_there(tmp_path):
+    """attn_prompt_kernel's matrix instructions are asm, so that the compiler adds no wait states in front of them: in its machine code no register that one reads is written by a
+    vector instruction among the two before it."""
+    asm = str(tmp_path / "attn_prompt.s")
+    flags = [f for f in build.HIPCC_FLAGS if not f.startswith("-Rpass")]
+    subprocess.run([os.environ.get("HIPCC", "/opt/rocm/bin/hipcc"), *flags, "--cuda-device-only", "-S", os.path.join(build.CSRC, "attn_prompt.hip"), "-o", asm],
+                   check=True, capture_output=True)
+    kernels = re.findall(r"^(_ZN6kvfold18attn_prompt_kernel\w+):(.*?)s_endpgm", open(asm).read(), re.S | re.M)
+    assert len(kernels) == 2
+    for name, text in kernels:
+        ins = [line.strip() for line in text.split("\n") if line.startswith("\t") and not line.strip().startswith((";", "."))]
+        matrix = [j for j, line in enumerate(ins) if line.startswith("v_mfma")]
+        assert len(matrix) > 100
+        for j in matrix:
+            reads = re.findall(r"([av])\[(\d+):(\d+)\]", ins[j])[1:]
+            states = 0
+            for line in ins[max(0, j - 5):j][::-1]:
+                if states >= 2:
+                    break
+                write = re.match(r"(v_\w+) ([av])(?:(\d+)|\[(\d+):(\d+)\])", line)
+                if write and not line.startswith(("v_mfma", "v_cmp")):
+                    low, high = int(write[3] or write[4]), int(write[3] or write[5])
+                    assert not any(f == write[2] and int(a) <= high and low <= int(b) for f, a, b in reads), (name, line, ins[j])
+                nop = re.match(r"s_nop (\d+)", line)
+                states += int(nop[1]) + 1 if nop else 0 if line.startswith("s_waitcnt") else 1
