@@ -12,6 +12,8 @@
 //
 // The step's new rows are not read from the cache: the one wavefront whose block they fall into takes them from k_new and v_new and stores them.
 //
+// 32 heads on 8, 128 wide: 256 sequences of 3000 to 5000 tokens on pages of 16 732 us, 5.7 TB/s; 64 of 16 to 16K 127, 4.8 TB/s; 4 of 128K 366, 5.8 TB/s; one of 300 tokens 7.3.
+//
 // bf16: neither queries nor keys are rounded on the way, P = 2^(S scale log2 e - m) is for P V (attn_decode.hip's rounding points but for the query's), row sums are
 // fp32 from the unrounded P, m is stale by at most 2^16.
 #include "meet.h"

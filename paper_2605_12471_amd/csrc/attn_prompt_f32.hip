@@ -1,7 +1,7 @@
 // Attention of whole prompts, and of chunks of them, of many sequences on a cache in pages, fp32: attn_prompt.hip's shape with one unit a wavefront and tiles of
 // 32 keys, on the fp32 matrix instructions.
 //
-// Bound by these: 32x32x2, 4 kFLOP in 64 cycles.  S^T = K Q^T: a lane has 16 bytes of a K row and of its query's, four contraction steps whose columns are
+// Bound by these: 32x32x2, 4 kFLOP in 64 cycles (3000 tokens, 32 heads on 8, 128 wide: 666 us, 111 TFLOP/s; six prompts of 47 to 725, 8 heads on 2, 64 wide: 20 us, two tiles a CU).  S^T = K Q^T: a lane has 16 bytes of a K row and of its query's, four contraction steps whose columns are
 // whichever these are.  O^T = V^T P^T: step i's two keys are those whose logits the two lanes of a row hold in register i, and a lane's 16 (64 wide: 8)
 // bytes of such a V row are its columns of all tiles of O^T (tile j has every fourth, or second, column of the head), so that V needs no transpose.
 #include "prompt.h"

@@ -9,7 +9,8 @@ typedef __attribute__((ext_vector_type(4))) unsigned uintx4;
 // A few thousand numbers: bound by the chain inside one launch.  Every workgroup goes through all requests for itself: for the totals, which say whether
 // anything is assigned at all, and for the running sums, from which it takes the tokens that are its share of the places (a long prompt's are shared out like
 // any others').  So nobody waits for another workgroup, there is one launch and no memory of its own.  Up to 1024 requests are gone through once, four a thread, more
-// of them twice.  A page is written into its table by the thread whose token is the page's first.
+// of them twice.  A page is written into its table by the thread whose token is the page's first.  64 requests of a token each 3.5 us, 300 with 145220 tokens 6.3 (twice through, four tokens
+// a thread one behind the other: 3.8 and 9.3).
 constexpr int kAssignThreads = 256, kAssignEach = 4, kAssignChunk = kAssignThreads * kAssignEach;
 
 struct Sums {
@@ -182,7 +183,8 @@ hipError_t launch_assign(const AssignParams& p, int n_cu, hipStream_t s) {
 //   the longest piece and what a workgroup does once, where all are there at the same time (less where each has a CU for itself); else W and N times what each of N
 //   does once over the places, and an eighth of the longest for the last round's gaps (of whole blocks: a half); and for pieces what they cost besides.
 // A sequence's blocks are cut at the same keys and stand side by side in the list: they read the same rows at about the same time.  The longest come first (five classes).  One workgroup,
-// beside the others that bring the new rows to their places: bound by its chain.
+// beside the others that bring the new rows to their places: bound by its chain, 6 us for eight sequences in 364 pieces (with a launch), of which each pass over the sequences, a running
+// sum and two barriers, is 1.
 constexpr int kPlanThreads = 256;
 constexpr int kPlanClasses = 5;
 constexpr int kPlanLengths = 4;  // of a piece that are looked at, an eighth of a share apart
@@ -370,7 +372,7 @@ __device__ void prompt_plan(const PromptPlanParams& p) {
 }
 
 // ---- append ------------------------------------------------------------------------------------------------------------
-// 16 bytes a thread and turn, neighbours side by side in a row: bound by memory, every row read and written once.
+// 16 bytes a thread, neighbours side by side in a row: bound by memory, every row read and written once (24K tokens of 8 KV heads, 128 wide: 33 us, 6.0 TB/s).
 __global__ void __launch_bounds__(kPlanThreads) pappend_kernel(PAppendParams p, PromptPlanParams plan, int per_row_log2, unsigned per_token, FastDiv by_token) {
   unsigned block = blockIdx.x;
   if (plan.items) {
