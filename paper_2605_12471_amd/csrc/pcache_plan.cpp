@@ -73,12 +73,14 @@ PagedPlan make_pplan(const kvfold_pcache_config_t& c, int n_cu, const kvfold_bat
     // as there are places, and those that the device's estimate of the tiles leaves out.
     pl.blocks = (int64_t)b.n_tokens * G / pl.unit_rows + std::min<int64_t>(b.n_seqs, b.n_tokens);
     pl.places = pl.units_per_wave == 2 ? n_cu : 2 * n_cu;
-    // (a tile of bf16, two units a wavefront: 1.6 us; of fp32, 64 wide, two workgroups a CU: 7)
-    pl.step = pl.units_per_wave == 2 ? 2 : 1;
+    // (a tile of bf16, two units a wavefront: 1.6 us; one, and two workgroups a CU: 2.8; of fp32, 64 wide, two workgroups a CU: 7)
+    // With what two units cost for one, too, short chunks stayed whole: 64 tokens on 900 keys 33.7 us, cut 21.9 (32 sequences of 20 to 60 on 20 to 900, cut or not, 38.6 and 39.9).
+    const bool two = pl.units_per_wave == 2;
+    pl.step = two ? 2 : 1;
     pl.shortest = bf16 ? 4 : 1;
-    pl.cost_once = bf16 ? 5 : 1;
-    pl.cost_piece = bf16 ? 8 : 0.5f;
-    pl.cost_merge = bf16 ? 8 : 1;
+    pl.cost_once = two ? 5 : bf16 ? 2 : 1;
+    pl.cost_piece = two ? 8 : bf16 ? 4 : 0.5f;
+    pl.cost_merge = two ? 8 : bf16 ? 1.5f : 1;
     const int64_t rows = (int64_t)b.n_tokens * c.n_q_heads;
     pieces = std::min<int64_t>({kPromptMaxPieces, steps, kPagedMaxRows / std::max<int64_t>(rows, 1)});
     // Whole prompts that fill the GPU are left in one piece: in bf16 the merge costs more than is won (1000 tokens, 32 heads on 8: 33.8 us, in pieces 38), in fp32 less (147, 114).
