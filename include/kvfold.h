@@ -500,7 +500,8 @@ typedef struct {
   uint32_t struct_size;  /* must be sizeof(kvfold_batch_t)                                                                      */
   int32_t n_seqs;        /* >= 0                                                                                                */
   int32_t n_tokens;      /* packed rows of q, k_new, v_new, out; those behind cu_new[n_seqs] are left alone                     */
-  int32_t max_new;       /* at least the new tokens of every sequence (tokens beyond are left alone)                            */
+  int32_t max_new;       /* at least the new tokens of every sequence (of one that has more, those beyond are left alone; the   */
+                         /* first max_new are what they would be under a bound that held)                                       */
   int64_t max_len;       /* at least every lens[s]; <= 2^30                                                                     */
   const int32_t* tables; /* device, [n_seqs][table_stride]                                                                      */
   int64_t table_stride;

@@ -56,7 +56,8 @@ KVFOLD_HD int paged_pieces(int len, int piece) {
 }
 
 // A sequence's new tokens and its length from what the device holds, inside the batch's bounds whatever that is: tokens [first, first + n) exist, n <= max_new,
-// 0 <= len <= max_len.
+// 0 <= len <= max_len.  Token i has the position len - n + i: where there are more than max_new, the length ends behind the last that counts (at 0, where that lies in front of
+// the first position).
 struct PagedSeq {
   int first, n, len;
 };
@@ -65,7 +66,9 @@ KVFOLD_HD PagedSeq paged_seq(int from, int to, int len, int n_tokens, int max_ne
   q.first = from < 0 ? 0 : from > n_tokens ? n_tokens : from;
   const int end = to < q.first ? q.first : to > n_tokens ? n_tokens : to;
   q.n = end - q.first < max_new ? end - q.first : max_new;
+  const int beyond = end - q.first - q.n;
   q.len = len < 0 ? 0 : len > max_len ? max_len : len;
+  q.len = q.len > beyond ? q.len - beyond : 0;
   return q;
 }
 
