@@ -492,14 +492,15 @@ int kvfold_pcache_assign(const kvfold_pcache_t* cache, int32_t n_seqs, const int
                          int32_t* n_free_after, int32_t* status, void* stream);
 
 /*
- * A batch: sequence s has the new tokens cu_new[s] .. cu_new[s + 1] - 1 of the packed rows, the last of its lens[s] tokens.  Sequences whose tokens overlap have no
- * defined results.  n_seqs <= 2^20, n_seqs * n_kv_heads <= 2^23, n_tokens * n_q_heads <= 2^28, n_tokens * q_stride <= 2^34, table_stride < 2^31, kv_stride <= 2^31, else
+ * A batch: sequence s has the new tokens cu_new[s] .. cu_new[s + 1] - 1 of the packed rows, the last of its lens[s] tokens (of more new tokens than that, the first ones
+ * have no position: they see nothing and are not stored).  Sequences whose tokens overlap have no defined results.  n_seqs <= 2^20, n_seqs * n_kv_heads <= 2^23, n_tokens * n_q_heads <= 2^28, n_tokens * q_stride <= 2^34, table_stride < 2^31, kv_stride <= 2^31, else
  * KVFOLD_ERR_UNSUPPORTED.
  */
 typedef struct {
   uint32_t struct_size;  /* must be sizeof(kvfold_batch_t)                                                                      */
   int32_t n_seqs;        /* >= 0                                                                                                */
-  int32_t n_tokens;      /* packed rows of q, k_new, v_new, out; those behind cu_new[n_seqs] are left alone                     */
+  int32_t n_tokens;      /* packed rows of q, k_new, v_new, out; those of no sequence, in front of cu_new[0] and behind         */
+                         /* cu_new[n_seqs], are left alone: no results, and not stored, whatever their places are               */
   int32_t max_new;       /* at least the new tokens of every sequence (of one that has more, those beyond are left alone; the   */
                          /* first max_new are what they would be under a bound that held)                                       */
   int64_t max_len;       /* at least every lens[s]; <= 2^30                                                                     */

@@ -72,6 +72,21 @@ KVFOLD_HD PagedSeq paged_seq(int from, int to, int len, int n_tokens, int max_ne
   return q;
 }
 
+// Whether packed token t is one of a sequence's that have a position.  The sequence is the last that begins at t or in front of it, of [s, hi) (the running sums ascend;
+// where they do not, some sequence in there).
+KVFOLD_HD bool paged_token(const int32_t* cu_new, const int32_t* lens, int s, int hi, int n_tokens, int max_new, int max_len, int t) {
+  while (hi - s > 1) {
+    const int mid = (int)((unsigned)(s + hi) >> 1);
+    if (cu_new[mid] <= t)
+      s = mid;
+    else
+      hi = mid;
+  }
+  const PagedSeq q = paged_seq(cu_new ? cu_new[s] : s, cu_new ? cu_new[s + 1] : s + 1, lens[s], n_tokens, max_new, max_len);
+  const int i = t - q.first;
+  return i >= 0 && i < q.n && i >= q.n - q.len;
+}
+
 }  // namespace kvfold
 
 #if defined(__HIP__)
@@ -101,6 +116,8 @@ struct PromptPlanParams {
 };
 struct PAppendParams {
   const void *k, *v;  // [n_tokens][Hkv][d] at token_bytes
+  const int32_t *lens, *cu_new;  // of the batch whose packed tokens [first, first + n_tokens) these are; lens = nullptr: the places alone decide
+  int32_t n_seqs, all_tokens, max_new, max_len, first;
   void *k_pages, *v_pages;
   const int64_t* slots;
   int64_t token_bytes;

@@ -38,9 +38,17 @@ bool all_apart(const Range& a, const Range* others, int n) {
 // Bytes of n tokens' rows of `heads` heads at `stride` elements
 size_t extent(int64_t n, int64_t stride, int64_t heads, int64_t d, int es) { return n < 1 ? 0 : ((size_t)(n - 1) * (size_t)stride + (size_t)(heads * d)) * (size_t)es; }
 
+// Rows to their places; `plan`: of the step that they are part of, whose sequences they have to belong to (lens = nullptr: of none)
 hipError_t append_rows(const kvfold_pcache* c, int layer, const void* k, const void* v, int64_t kv_stride, const int64_t* slots, int32_t n, const PromptPlanParams& plan,
                        hipStream_t s) {
   PAppendParams p;
+  p.lens = plan.lens;
+  p.cu_new = plan.cu_new;
+  p.n_seqs = plan.n_seqs;
+  p.all_tokens = plan.n_tokens;
+  p.max_new = plan.max_new;
+  p.max_len = plan.max_len;
+  p.first = 0;
   p.k = k;
   p.v = v;
   p.k_pages = c->rows(layer, false);

@@ -31,7 +31,34 @@ static void positions() {
         }
 }
 
+// A token belongs to the sequence that holds it, if it has a position there and counts; running sums that do not ascend end the search inside them.
+static void tokens() {
+  std::mt19937 rng(5);
+  auto any = [&](int lo, int hi) { return lo + (int)(rng() % (unsigned)(hi - lo + 1)); };
+  for (int i = 0; i < 3000; ++i) {
+    const int seqs = any(1, 40), lead = any(0, 3), max_new = any(1, 9);
+    std::vector<int32_t> cu(seqs + 1), lens(seqs);
+    cu[0] = lead;
+    for (int s = 0; s < seqs; ++s) {
+      cu[s + 1] = cu[s] + (any(0, 2) ? any(0, 12) : 0);
+      lens[s] = any(0, 20);
+    }
+    const int n_tokens = cu[seqs] + any(0, 4);
+    for (int t = 0; t < n_tokens; ++t) {
+      bool want = false;
+      for (int s = 0; s < seqs; ++s)
+        if (cu[s] <= t && t < cu[s + 1]) want = t - cu[s] < max_new && lens[s] - (cu[s + 1] - t) >= 0;
+      CHECK(paged_token(cu.data(), lens.data(), 0, seqs, n_tokens, max_new, 1000, t) == want);
+    }
+    for (int t = 0; t < seqs; ++t) CHECK(paged_token(nullptr, lens.data(), t, t + 1, seqs, 1, 1000, t) == (lens[t] > 0));
+    for (auto& x : cu) x = any(0, 3) ? any(-5, 60) : any(0, 1) ? INT32_MIN : INT32_MAX;
+    for (auto& x : lens) x = any(0, 3) ? any(-5, 60) : any(0, 1) ? INT32_MIN : INT32_MAX;
+    for (int t = 0; t < n_tokens; ++t) (void)paged_token(cu.data(), lens.data(), 0, seqs, n_tokens, max_new, 1000, t);
+  }
+}
+
 int main() {
   positions();
-  std::puts("ok: positions");
+  tokens();
+  std::puts("ok: positions, tokens");
 }
