@@ -1024,16 +1024,16 @@ class KvFoldBatch:
         self.max_new, self.max_len = max_new, max_len
         where = f"cuda:{dev}"
 
-        def mine(name, given, shape, dtype):
+        def mine(name, given, shape, dtype, value=0):
             if given is None:
-                return torch.zeros(shape, dtype=dtype, device=where)
+                return torch.full(shape, value, dtype=dtype, device=where)
             _expect(name, given, dtype, dev, shape)
             return given
         if not (0 <= n_tokens < 1 << 31 and 1 <= max_new < 1 << 31 and 1 <= max_len <= 1 << 30):
             raise ValueError(f"a batch of {n_tokens} tokens, max_new {max_new}, max_len {max_len} is none")
         self.lens = mine("lens", lens, (self.n_seqs,), torch.int32)
         self.cu_new = mine("cu_new", cu_new, (self.n_seqs + 1,), torch.int32)
-        self.slots = mine("slots", slots, (n_tokens,), torch.int64)
+        self.slots = mine("slots", slots, (n_tokens,), torch.int64, -1)  # (no place, until one is given)
         self.positions, self.n_free, self.status = (torch.zeros(shape, dtype=torch.int32, device=where) for shape in ((n_tokens,), (1,), (1,)))
         need = kvfold_pcache_workspace_bytes(cache.handle, make_batch(self.n_seqs, n_tokens, max_new, max_len, tables.data_ptr(), tables.shape[1], None, None, None))
         if not need:
