@@ -516,7 +516,7 @@ typedef struct {
 
 /*
  * Bytes of device memory that kvfold_pcache_step needs for a batch of these numbers (pointers are not looked at).  They have to be zero before the
- * first use, and every call leaves them so that others with the same n_seqs can follow.  Host-only; 0 for an invalid batch.
+ * first use, and every call leaves them so that others with the same n_seqs, on caches with the same n_kv_heads, can follow.  Host-only; 0 for an invalid batch.
  */
 size_t kvfold_pcache_workspace_bytes(const kvfold_pcache_t* cache, const kvfold_batch_t* batch /* host */);
 

@@ -943,12 +943,14 @@ class KvFoldPagedCache:
         """Enqueue one fold step of every sequence of the batch: q, out [n_tokens][Hq][d], k_new, v_new [n_tokens][Hkv][d], lse fp32 [Hq][n_tokens].  q, k_new and v_new
         may be parts of one tensor.  k_new = v_new = None: the new rows are in the pages already (``append``)."""
         n = batch.n_tokens
+        if batch.cache is not self and batch.cache._hkv != self._hkv:  # (its workspace has a counter for each sequence and KV head)
+            raise ValueError(f"batch: made for {batch.cache._hkv} KV heads, the cache has {self._hkv}")
         bound = self._bound
         if bound is False:
             bound = self._bind()
         if bound is not None:
-            rc = _native.paged_step(bound, layer, batch.tables, batch.lens, None if batch.one_each else batch.cu_new, batch.slots, batch.workspace, n, batch.max_new,
-                                    batch.max_len, q, k_new, v_new, out, lse, stream)
+            rc = _native.paged_step(bound, layer, batch.n_seqs, batch.tables, batch.lens, None if batch.one_each else batch.cu_new, batch.slots, batch.workspace, n,
+                                    batch.max_new, batch.max_len, q, k_new, v_new, out, lse, stream)
             if rc == 0:
                 return out
             if rc is not None:
@@ -1012,6 +1014,7 @@ class KvFoldBatch:
 
     n_tokens rows are packed in a step's tensors; max_new and max_len bound the new tokens and the tokens of any sequence.  one_each: every sequence has
     exactly one new token, and n_tokens = n_seqs.  A batch is good for one step at a time: steps that may overlap (on streams of their own) have a batch each.
+    Its workspace is for its number of sequences and its cache's of KV heads: a step on another cache has to have as many.
     What is made here is made on the current stream: a step on another one waits for it."""
 
     def __init__(self, cache, tables, n_tokens, max_new, max_len, lens=None, cu_new=None, slots=None, one_each=False):

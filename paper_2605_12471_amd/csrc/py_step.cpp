@@ -374,21 +374,22 @@ bool table_of(PyObject* obj, int64_t* rows, int64_t* columns) {
 }
 int64_t numel_of(PyObject* obj) { return THPVariable_CheckExact(obj) && THPVariable_Unpack(obj).defined() ? THPVariable_Unpack(obj).numel() : -1; }
 
-// paged_step(cache, layer, tables, lens, cu_new or None, slots, workspace, n_tokens, max_new, max_len, q, k_new, v_new, out, lse, stream)
+// paged_step(cache, layer, n_seqs, tables, lens, cu_new or None, slots, workspace, n_tokens, max_new, max_len, q, k_new, v_new, out, lse, stream)
 PyObject* paged_step(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
-  if (n_args != 16) {
-    PyErr_SetString(PyExc_TypeError, "paged_step: 16 arguments");
+  if (n_args != 17) {
+    PyErr_SetString(PyExc_TypeError, "paged_step: 17 arguments");
     return nullptr;
   }
   const Paged* c = static_cast<Paged*>(PyCapsule_GetPointer(a[0], "kvfold_paged"));
   if (!c) return nullptr;
   try {
-    int64_t layer, n, max_new, max_len, seqs, columns, q_stride, kv_stride = 0, v_stride = 0;
-    if (!whole_number(a[1], INT32_MIN, INT32_MAX, &layer) || !whole_number(a[7], 1, INT32_MAX, &n) || !whole_number(a[8], INT32_MIN, INT32_MAX, &max_new) ||
-        !whole_number(a[9], INT64_MIN, INT64_MAX, &max_len) || !table_of(a[2], &seqs, &columns) || seqs < 1)
+    int64_t layer, n, max_new, max_len, n_seqs, seqs, columns, q_stride, kv_stride = 0, v_stride = 0;
+    if (!whole_number(a[1], INT32_MIN, INT32_MAX, &layer) || !whole_number(a[8], 1, INT32_MAX, &n) || !whole_number(a[9], INT32_MIN, INT32_MAX, &max_new) ||
+        !whole_number(a[10], INT64_MIN, INT64_MAX, &max_len) || !whole_number(a[2], 1, INT32_MAX, &n_seqs) || !table_of(a[3], &seqs, &columns) ||
+        seqs != n_seqs)
       Py_RETURN_NONE;
     constexpr auto i32 = c10::ScalarType::Int, i64 = c10::ScalarType::Long;
-    const int64_t table[2] = {seqs, columns}, each[1] = {seqs}, sums[1] = {seqs + 1}, tokens[1] = {n}, bytes[1] = {numel_of(a[6])};
+    const int64_t table[2] = {seqs, columns}, each[1] = {seqs}, sums[1] = {seqs + 1}, tokens[1] = {n}, bytes[1] = {numel_of(a[7])};
     const int64_t wide[3] = {n, c->n_q_heads, c->head_dim}, per_head[2] = {c->n_q_heads, n};
     bool ok = true;
     kvfold_batch_t b;
@@ -397,21 +398,21 @@ PyObject* paged_step(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     b.n_tokens = (int32_t)n;
     b.max_new = (int32_t)max_new;
     b.max_len = max_len;
-    b.tables = static_cast<int32_t*>(plain(a[2], c->device, i32, table));
+    b.tables = static_cast<int32_t*>(plain(a[3], c->device, i32, table));
     b.table_stride = columns;
-    b.lens = static_cast<int32_t*>(plain(a[3], c->device, i32, each));
-    b.cu_new = static_cast<int32_t*>(plain_or_none(a[4], c->device, i32, sums, &ok));
+    b.lens = static_cast<int32_t*>(plain(a[4], c->device, i32, each));
+    b.cu_new = static_cast<int32_t*>(plain_or_none(a[5], c->device, i32, sums, &ok));
     b.slots = nullptr;
-    void *space = plain(a[6], c->device, c10::ScalarType::Byte, bytes), *q = rows_with_stride(a[10], *c, n, c->n_q_heads, &q_stride), *k = nullptr, *v = nullptr,
-         *out = plain(a[13], c->device, c->dtype, wide), *stream;
-    float* lse = static_cast<float*>(plain_or_none(a[14], c->device, c10::ScalarType::Float, per_head, &ok));
-    if (a[11] != Py_None || a[12] != Py_None) {
-      k = rows_with_stride(a[11], *c, n, c->n_kv_heads, &kv_stride);
-      v = rows_with_stride(a[12], *c, n, c->n_kv_heads, &v_stride);
-      b.slots = static_cast<int64_t*>(plain(a[5], c->device, i64, tokens));
+    void *space = plain(a[7], c->device, c10::ScalarType::Byte, bytes), *q = rows_with_stride(a[11], *c, n, c->n_q_heads, &q_stride), *k = nullptr, *v = nullptr,
+         *out = plain(a[14], c->device, c->dtype, wide), *stream;
+    float* lse = static_cast<float*>(plain_or_none(a[15], c->device, c10::ScalarType::Float, per_head, &ok));
+    if (a[12] != Py_None || a[13] != Py_None) {
+      k = rows_with_stride(a[12], *c, n, c->n_kv_heads, &kv_stride);
+      v = rows_with_stride(a[13], *c, n, c->n_kv_heads, &v_stride);
+      b.slots = static_cast<int64_t*>(plain(a[6], c->device, i64, tokens));
       ok = ok && k && v && b.slots && kv_stride == v_stride;
     }
-    if (!ok || !b.tables || !b.lens || !space || !q || !out || !stream_of(a[15], c->device, &stream)) Py_RETURN_NONE;
+    if (!ok || !b.tables || !b.lens || !space || !q || !out || !stream_of(a[16], c->device, &stream)) Py_RETURN_NONE;
     b.q_stride = q_stride;
     b.kv_stride = kv_stride;
     int rc;
