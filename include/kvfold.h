@@ -507,7 +507,9 @@ typedef struct {
   const int32_t* tables; /* device, [n_seqs][table_stride]                                                                      */
   int64_t table_stride;
   const int32_t* lens;   /* device, [n_seqs]: tokens of each sequence, the new ones among them                                  */
-  const int32_t* cu_new; /* device, [n_seqs + 1]; or NULL: token s is the only new one of sequence s (n_tokens = n_seqs)        */
+  const int32_t* cu_new; /* device, [n_seqs + 1]; or NULL: token s is the only new one of sequence s (n_tokens = n_seqs), with   */
+                         /* slots only if its place is in the cache (kvfold_pcache_assign gives none where its status is not 0; */
+                         /* without slots nothing tells a step of that)                                                         */
   const int64_t* slots;  /* device, [n_tokens]: places of the new rows, those of the tables; or NULL, with k_new and v_new: they */
                          /* are there already (kvfold_pcache_append)                                                            */
   int64_t q_stride;      /* elements from a token's q to the next one's, a multiple of 8 (f32: 4); 0: n_q_heads * head_dim        */

@@ -1013,7 +1013,8 @@ class KvFoldBatch:
     given: lens int32 [n_seqs] (the new tokens among them), cu_new int32 [n_seqs + 1], slots int64 [n_tokens], and the workspace of its steps.
 
     n_tokens rows are packed in a step's tensors; max_new and max_len bound the new tokens and the tokens of any sequence.  one_each: every sequence has
-    exactly one new token, and n_tokens = n_seqs.  A batch is good for one step at a time: steps that may overlap (on streams of their own) have a batch each.
+    exactly one new token, and n_tokens = n_seqs (a sequence whose place is none, as after an assign whose status is not 0, has no new token; a step without k_new and
+    v_new does not look at places).  A batch is good for one step at a time: steps that may overlap (on streams of their own) have a batch each.
     Its workspace is for its number of sequences and its cache's of KV heads: a step on another cache has to have as many.
     What is made here is made on the current stream: a step on another one waits for it."""
 

@@ -87,6 +87,10 @@ __global__ void __launch_bounds__(kPDecodeWaves * 64, 2) attn_pdecode_kernel(PAt
     }
     sq = paged_seq(from, to, len, p.n_tokens, p.max_new, p.max_len);
   }
+  // The place of the one token, where there are no running sums (paged_one): asked for behind the lengths, and not waited for before it is needed (16 unlike sequences 24.2 us, in front of the
+  // lengths' use 26.5, without it 23.9).
+  int64_t place = 0;
+  if (!p.cu_new && p.slots) place = ((ConstPtr<int64_t>)(uintptr_t)p.slots)[seq];
   int piece_keys = p.piece;
   if (p.shared != 0.f) {  // a workgroup's share of all keys: every workgroup adds up all lengths, which come with its own
     int steps = 0;        // (of 128 keys: a sum of fewer than 2^31)
@@ -98,7 +102,7 @@ __global__ void __launch_bounds__(kPDecodeWaves * 64, 2) attn_pdecode_kernel(PAt
     piece_keys = share > piece_keys ? share : piece_keys;
   }
   const int n_pieces = paged_pieces(sq.len, piece_keys);
-  if (sq.n == 0 || piece >= n_pieces) return;
+  if (sq.n == 0 || piece >= n_pieces || (uint64_t)place >= (uint64_t)p.n_places) return;
 
   const int Hq = p.n_q_heads, G = p.group, rows = sq.n * G, prev = sq.len - sq.n;
 

@@ -72,6 +72,10 @@ KVFOLD_HD PagedSeq paged_seq(int from, int to, int len, int n_tokens, int max_ne
   return q;
 }
 
+// Without running sums: the end of sequence s's tokens, which begin at s.  It has one, where rows are stored (slots) if that has a place: an assignment that could not be made
+// leaves it none.
+KVFOLD_HD int paged_one(const int64_t* slots, int64_t n_places, int s) { return slots && (uint64_t)slots[s] >= (uint64_t)n_places ? s : s + 1; }
+
 // Whether packed token t is one of a sequence's that have a position.  The sequence is the last that begins at t or in front of it, of [s, hi) (the running sums ascend;
 // where they do not, some sequence in there).
 KVFOLD_HD bool paged_token(const int32_t* cu_new, const int32_t* lens, int s, int hi, int n_tokens, int max_new, int max_len, int t) {
@@ -106,6 +110,8 @@ hipError_t launch_assign(const AssignParams& p, int n_cu, hipStream_t s);
 // The list of a batch's work, made by one workgroup
 struct PromptPlanParams {
   const int32_t *lens, *cu_new;
+  const int64_t* slots;  // nullptr: nothing is stored
+  int64_t all_places;    // of the cache
   int32_t* head;      // [0] items, [1] blocks to merge
   PromptItem* items;  // nullptr: no list is asked for
   int32_t* merges;    // behind them: the first pieces of blocks that have several

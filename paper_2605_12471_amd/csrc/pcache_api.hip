@@ -275,6 +275,8 @@ int kvfold_pcache_step(const kvfold_pcache_t* c, int layer, const kvfold_batch_t
     PromptPlanParams plan;
     plan.lens = b->lens;
     plan.cu_new = b->cu_new;
+    plan.slots = b->slots;
+    plan.all_places = c->places();
     plan.head = reinterpret_cast<int32_t*>(list);
     plan.items = reinterpret_cast<PromptItem*>(list + kPromptHead);
     plan.n_seqs = b->n_seqs;

@@ -209,7 +209,7 @@ __device__ void prompt_plan(const PromptPlanParams& p) {
   auto chunk = [&](int s0) -> PlanSums {
     const int s = s0 + tid;
     PagedSeq q = {0, 0, 0};
-    if (s < p.n_seqs) q = paged_seq(p.cu_new ? p.cu_new[s] : s, p.cu_new ? p.cu_new[s + 1] : s + 1, p.lens[s], p.n_tokens, p.max_new, p.max_len);
+    if (s < p.n_seqs) q = paged_seq(p.cu_new ? p.cu_new[s] : s, p.cu_new ? p.cu_new[s + 1] : paged_one(p.slots, p.all_places, s), p.lens[s], p.n_tokens, p.max_new, p.max_len);
     const int nb = blocks_of(q);
     const int keys = q.len - q.n / 2;  // of a block, about
     const int64_t tiles = wave_scan((int64_t)nb * ((keys > 0 ? keys : 0) / 64 + 1)), blocks = wave_scan((int64_t)nb);

@@ -51,6 +51,8 @@ static void tokens() {
       CHECK(paged_token(cu.data(), lens.data(), 0, seqs, n_tokens, max_new, 1000, t) == want);
     }
     for (int t = 0; t < seqs; ++t) CHECK(paged_token(nullptr, lens.data(), t, t + 1, seqs, 1, 1000, t) == (lens[t] > 0));
+    const int64_t slots[] = {0, 99, 100, -1, INT64_MIN, INT64_MAX};
+    for (int t = 0; t < 6; ++t) CHECK(paged_one(slots, 100, t) == (t < 2 ? t + 1 : t) && paged_one(nullptr, 100, t) == t + 1);
     for (auto& x : cu) x = any(0, 3) ? any(-5, 60) : any(0, 1) ? INT32_MIN : INT32_MAX;
     for (auto& x : lens) x = any(0, 3) ? any(-5, 60) : any(0, 1) ? INT32_MIN : INT32_MAX;
     for (int t = 0; t < n_tokens; ++t) (void)paged_token(cu.data(), lens.data(), 0, seqs, n_tokens, max_new, 1000, t);
