@@ -877,10 +877,16 @@ __global__ void __launch_bounds__(256, 1) attn_prompt_kernel(PAttnParams p) {
         }
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) mfma_settle_v(sA[qb]);
-        if (t_begin * BN + 32 > vis_min || t_begin >= t_bad) mask_half(sA, 2 * t_begin);
+        const bool whole = t_begin * BN + 32 <= vis_min && t_begin < t_bad;
+        if (!whole) mask_half(sA, 2 * t_begin);
         float mx[QB];
         rowmax_all(sA, mx);
         reference_first(mx, sA);
+        // A row whose 32 logits are all -inf, none of them masked, has no reference, and the main loop finds none: the exact pass does.
+        if (whole) {
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) overflowed |= __any((int)(m_run[qb] == -INFINITY));
+        }
         if (t_begin >= t_dead && t_dead < t_end)
           early_events(sA, std::integral_constant<int, QB - 1>{});  // the first step already works on unit 1 alone
         else
