@@ -510,8 +510,8 @@ typedef struct {
   const int32_t* cu_new; /* device, [n_seqs + 1]; or NULL: token s is the only new one of sequence s (n_tokens = n_seqs), with   */
                          /* slots only if its place is in the cache (kvfold_pcache_assign gives none where its status is not 0; */
                          /* without slots nothing tells a step of that)                                                         */
-  const int64_t* slots;  /* device, [n_tokens]: places of the new rows, those of the tables; or NULL, with k_new and v_new: they */
-                         /* are there already (kvfold_pcache_append)                                                            */
+  const int64_t* slots;  /* device, [n_tokens]: places of the new rows, those of the tables, no two the same (else what lies     */
+                         /* there is a mixture); or NULL, with k_new and v_new: they are there already (kvfold_pcache_append)   */
   int64_t q_stride;      /* elements from a token's q to the next one's, a multiple of 8 (f32: 4); 0: n_q_heads * head_dim        */
   int64_t kv_stride;     /* the same of k_new and v_new; 0: n_kv_heads * head_dim                                               */
 } kvfold_batch_t;
@@ -537,7 +537,7 @@ size_t kvfold_pcache_workspace_bytes(const kvfold_pcache_t* cache, const kvfold_
 int kvfold_pcache_step(const kvfold_pcache_t* cache, int layer, const kvfold_batch_t* batch /* host */, const void* q, const void* k_new, const void* v_new,
                        void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Rows to their places without attention: k, v and slots as for the step, kv_stride 0 for dense rows. */
+/* Rows to their places without attention, those with a place in the cache: k, v and slots as for the step, kv_stride 0 for dense rows. */
 int kvfold_pcache_append(const kvfold_pcache_t* cache, int layer, const void* k, const void* v, int64_t kv_stride, const int64_t* slots, int32_t n_tokens,
                          void* stream);
 

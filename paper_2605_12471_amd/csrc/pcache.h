@@ -12,7 +12,7 @@ constexpr int64_t kPagedMaxRows = 1 << 20;  // (row, piece) pairs of a workspace
 constexpr int kPagedMeetStride = 16;        // words from one unit's counter to the next: a line's
 constexpr int kPagedMaxPieces = 128;        // of a sequence's keys
 constexpr int kPagedLongestPiece = 2048;    // keys (decode)
-constexpr int64_t kPagedMostWgs = 2048;     // of a decoding step whose lengths decide: many find that they have no piece (4096: 27.1 us for the first 24.2 in pcache_plan.cpp, 1024: 27.0)
+constexpr int64_t kPagedMostWgs = 2048;     // of a decoding step whose lengths decide: many find that they have no piece (4096: 27.1 us for the first 24.2 in pcache_plan.cpp, 1024: 27.0; under a max_len that was the longest sequence's)
 
 int validate_pconfig(const kvfold_pcache_config_t* c);
 size_t pcache_layer_bytes(const kvfold_pcache_config_t& c);  // K and V
